@@ -26,7 +26,11 @@
  *                        its KV cache, with the LSE;
  *   apb_merge_partials   MergeScore of the hosts' partial results;
  * plus apb_decode_attention_noalloc, the decode call for callers that cannot
- * allocate (its scratch is the library's own).
+ * allocate (its scratch is the library's own), and the same stage over a KV
+ * cache held in 4 bits, a quarter of the bytes:
+ *   apb_cache4_write     quantise K and V rows into the cache;
+ *   apb_cache4_read      read rows of it back in bf16;
+ *   apb_decode4_attention  one host's attention of the new tokens over it.
  *
  * Conventions shared by every entry point
  *   - All tensor pointers are caller-owned DEVICE memory on the current HIP
@@ -279,6 +283,120 @@ apb_status_t apb_decode_attention_noalloc(const apb_decode_problem_t* p, const u
 apb_status_t apb_merge_partials(int32_t n_parts, int32_t rows, int32_t head_dim,
                                 const float* o_parts, const float* lse_parts, uint16_t* o,
                                 float* lse, void* stream);
+
+/* ------------------------------------------------------------------------
+ * KV cache in 4 bits.  A host's decoding step reads its whole cache once per
+ * token; in 4 bits that is 0.53 bytes an element in place of 2.  Elements are
+ * e2m1 (sign, two exponent bits, one mantissa bit: magnitudes 0, 0.5, 1, 1.5, 2,
+ * 3, 4, 6), in groups of 32 along the head size that share one power of two
+ * (the OCP microscaling format MXFP4):
+ *   codes   uint8 [n_kv][capacity][d / 2]   element 2j of a row in the low half
+ *                                           of byte j, element 2j + 1 in the high
+ *   scales  uint8 [n_kv][capacity][d / 32]  byte b of a group: its elements are
+ *                                           their code's value times 2^(b - 127);
+ *                                           b = 255: all 32 are NaN
+ * for K and for V.  capacity is the rows per head that there is room for, so
+ * that tokens can be appended in place.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  uint8_t* k_codes;   /* [n_kv][capacity][d / 2]   16-byte aligned            */
+  uint8_t* k_scales;  /* [n_kv][capacity][d / 32]  4-byte aligned             */
+  uint8_t* v_codes;   /* as k_codes                                           */
+  uint8_t* v_scales;  /* as k_scales                                          */
+} apb_cache4_t;
+
+/* Which rows a write or a read moves between the cache and bf16 tensors of
+ * bf16_rows rows per head (rows bf16_first .. of every head; a layer's K/V with
+ * its anchor rows before the local block, say). */
+typedef struct {
+  int32_t n_kv_heads; /* 1 <= n_kv <= 65536                                   */
+  int32_t head_dim;   /* d, in {64, 128}                                      */
+  int32_t capacity;   /* 1 .. 2^30 rows per head of the cache                 */
+  int32_t first_row;  /* >= 0: first cache row                                */
+  int32_t n_rows;     /* >= 0: rows; first_row + n_rows <= capacity           */
+  int32_t bf16_rows;  /* 0 .. 2^30 rows per head of the bf16 tensors          */
+  int32_t bf16_first; /* >= 0: their first row; + n_rows <= bf16_rows         */
+} apb_cache4_problem_t;
+
+/* Host-only checks of a cache problem (no HIP call). */
+apb_status_t apb_validate_cache4(const apb_cache4_problem_t* p);
+
+/*
+ * apb_cache4_write -- quantise rows of K and V into the cache.
+ *
+ *   k, v    bf16 [n_kv][bf16_rows][d]
+ *   cache   its rows first_row .. first_row + n_rows - 1 of every head are
+ *           written, and nothing else.
+ * A group with largest magnitude a takes the smallest e in -120 .. 125 with
+ * a <= 7 * 2^e (e = 125 where none has it) and b = e + 127; its elements are
+ * x * 2^-e rounded to nearest, ties to the even code, magnitudes past 6 to 6,
+ * the sign kept (also of zeros).  A group with an infinity or a NaN gets b = 255
+ * and codes of zero: it reads back as NaN, never as finite numbers.  The bytes
+ * are a function of the row alone: the same in every call and for any n_rows.
+ * n_rows == 0 launches nothing and returns APB_OK (pointers may be NULL).
+ */
+apb_status_t apb_cache4_write(const apb_cache4_problem_t* p, const uint16_t* k,
+                              const uint16_t* v, const apb_cache4_t* cache, void* stream);
+
+/*
+ * apb_cache4_read -- the values of cache rows first_row .. first_row + n_rows - 1
+ * into rows bf16_first .. of k and v (bf16 [n_kv][bf16_rows][d]; their other rows
+ * are left alone).  Exact: a value has two significant bits.  Scale bytes that
+ * apb_cache4_write does not write (0 .. 6, 253, 254) lie past bf16's normal
+ * numbers and read back as unspecified values, except that codes of zero
+ * under b = 0 (memory set to zero) are zeros.
+ */
+apb_status_t apb_cache4_read(const apb_cache4_problem_t* p, const apb_cache4_t* cache,
+                             uint16_t* k, uint16_t* v, void* stream);
+
+/* One host's decoding step over a cache in 4 bits. */
+typedef struct {
+  int32_t n_q_heads;  /* n_q >= 1, a multiple of n_kv                        */
+  int32_t n_kv_heads; /* 1 <= n_kv <= 65536; query head i reads KV head
+                         i / (n_q/n_kv)                                      */
+  int32_t head_dim;   /* d, in {64, 128}                                     */
+  int32_t capacity;   /* 1 .. 2^30 rows per head that the cache has room for */
+  int32_t cache_len;  /* 0 <= Lc <= capacity: the rows that hold keys        */
+  int32_t n_new;      /* >= 1 new tokens                                     */
+  int32_t causal;     /* 1 on the last host, whose cache already ends with the
+                         new tokens' own rows (Lc >= n_new): new token j sees
+                         rows 0 .. Lc - n_new + j; 0: every row of Lc        */
+} apb_decode4_problem_t;
+
+/* Host-only checks of a decode problem over a 4-bit cache (no HIP call). */
+apb_status_t apb_validate_decode4(const apb_decode4_problem_t* p);
+
+/* Bytes of device workspace apb_decode4_attention needs for `p` (host only;
+ * depends on the shapes only). */
+apb_status_t apb_decode4_workspace_size(const apb_decode4_problem_t* p, uint64_t* bytes);
+
+/*
+ * apb_decode4_attention -- apb_decode_attention over a cache in 4 bits, the new
+ * tokens' own rows (on the last host) being part of it: apb_cache4_write them
+ * first.
+ *
+ *   q        bf16 [n_q][n_new][d]   the new tokens' queries.
+ *   cache    rows 0 .. Lc-1 of every head are read; ignored (may be NULL, its
+ *            pointers too) when Lc == 0.  Rows past Lc, and for a new token the
+ *            rows that it does not see, have no part in the result, whatever
+ *            they hold.
+ *   o_part   fp32 [n_q][n_new][d]   this host's partial output A_h, as
+ *   lse_part fp32 [n_q][n_new]      apb_merge_partials takes them; a row with no
+ *                                   visible key gets o = 0, lse = -inf.
+ *   softmax_scale  as in apb_attention_fwd.
+ *   workspace, workspace_bytes  caller-owned device scratch of at least
+ *                   apb_decode4_workspace_size() bytes, 16-byte aligned; the
+ *                   call overwrites it (calls that overlap in time must not
+ *                   share one).  The library allocates nothing.
+ * Arithmetic: bf16 queries against the cache's exact values, fp32 dot products
+ * and softmax, fp32 accumulation and output.  A NaN among a row's visible logits
+ * makes its o and lse NaN; a NaN group of a visible V row makes its 32 output
+ * elements NaN.
+ */
+apb_status_t apb_decode4_attention(const apb_decode4_problem_t* p, const uint16_t* q,
+                                   const apb_cache4_t* cache, float* o_part, float* lse_part,
+                                   float softmax_scale, void* workspace,
+                                   uint64_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * One host's whole layer (Alg. 2): the QKV projection of the anchor and

@@ -20,6 +20,11 @@ from .decode_oracle import (  # noqa: F401
     merge_ref,
     stage2_ref,
 )
+from .cache4_oracle import (  # noqa: F401
+    quantise4_ref,
+    values4_ref,
+    decode4_ref,
+)
 from .scorer_oracle import (  # noqa: F401
     scorer_features,
     silu,

@@ -24,7 +24,9 @@ EXPORTED = ("apb_compress_select", "apb_attention_fwd", "apb_validate_problem",
             "apb_decode_attention_noalloc",
             "apb_merge_partials", "apb_validate_scorer", "apb_scorer_workspace_size",
             "apb_retaining_scores", "apb_validate_layer", "apb_layer_workspace_size",
-            "apb_layer_flops", "apb_layer_fwd")
+            "apb_layer_flops", "apb_layer_fwd", "apb_validate_cache4", "apb_cache4_write",
+            "apb_cache4_read", "apb_validate_decode4", "apb_decode4_workspace_size",
+            "apb_decode4_attention")
 
 
 class ApbError(RuntimeError):
@@ -98,6 +100,32 @@ class LayerWeights(ctypes.Structure):
                                                "w_down", "r_w1", "r_b1", "r_w2", "r_b2")]
 
 
+class Cache4(ctypes.Structure):
+    """``apb_cache4_t``: device pointers of a KV cache in 4 bits."""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")]
+
+
+class Cache4Problem(ctypes.Structure):
+    """``apb_cache4_problem_t``: the rows that a write to, or a read of, a KV
+    cache in 4 bits moves."""
+
+    _fields_ = [("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("capacity", ctypes.c_int32), ("first_row", ctypes.c_int32),
+                ("n_rows", ctypes.c_int32), ("bf16_rows", ctypes.c_int32),
+                ("bf16_first", ctypes.c_int32)]
+
+
+class Decode4Problem(ctypes.Structure):
+    """``apb_decode4_problem_t``: one host's decoding step over a KV cache in
+    4 bits."""
+
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("capacity", ctypes.c_int32),
+                ("cache_len", ctypes.c_int32), ("n_new", ctypes.c_int32),
+                ("causal", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -156,6 +184,21 @@ def lib() -> ctypes.CDLL:
         L.apb_layer_fwd.argtypes = [lp_, ctypes.POINTER(LayerWeights), vp, vp, vp, vp, vp, vp, vp,
                                     vp, ctypes.c_uint64, vp]
         L.apb_layer_fwd.restype = ctypes.c_int
+        cp, c4 = ctypes.POINTER(Cache4Problem), ctypes.POINTER(Cache4)
+        L.apb_validate_cache4.argtypes = [cp]
+        L.apb_validate_cache4.restype = ctypes.c_int
+        L.apb_cache4_write.argtypes = [cp, vp, vp, c4, vp]
+        L.apb_cache4_write.restype = ctypes.c_int
+        L.apb_cache4_read.argtypes = [cp, c4, vp, vp, vp]
+        L.apb_cache4_read.restype = ctypes.c_int
+        d4 = ctypes.POINTER(Decode4Problem)
+        L.apb_validate_decode4.argtypes = [d4]
+        L.apb_validate_decode4.restype = ctypes.c_int
+        L.apb_decode4_workspace_size.argtypes = [d4, ctypes.POINTER(ctypes.c_uint64)]
+        L.apb_decode4_workspace_size.restype = ctypes.c_int
+        L.apb_decode4_attention.argtypes = [d4, vp, c4, vp, vp, ctypes.c_float, vp,
+                                            ctypes.c_uint64, vp]
+        L.apb_decode4_attention.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -365,3 +408,95 @@ def layer_fwd(problem, weights: dict, hidden_in, positions, k_cache, v_cache, pa
         _ptr(hidden_out, "hidden_out", b), workspace.data_ptr(),
         workspace.numel() * workspace.element_size(), _stream(stream))
     _check(st, "apb_layer_fwd")
+
+
+# The elements that a call's sizes ask of each tensor are counted here: a cache
+# is sized by its capacity, not by the rows in use, so a tensor of another size
+# is an easy mistake, and one that the C call cannot see.  Nor can it see a tensor
+# of another device than the current one, whose stream the call would use.
+def _sized(t, name, dtypes, n):
+    ptr = _ptr(t, name, dtypes)
+    if t is not None:
+        if t.numel() != n:
+            raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
+        _on_current_device(t, name)
+    return ptr
+
+
+def _on_current_device(t, name):
+    import torch
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+
+
+def _cache4(cache, n_kv, capacity, d):
+    """``apb_cache4_t`` of a mapping of the four tensors (uint8)."""
+    import torch
+    u, c = (torch.uint8,), Cache4()
+    for name, n in (("k_codes", d // 2), ("k_scales", d // 32), ("v_codes", d // 2),
+                    ("v_scales", d // 32)):
+        setattr(c, name, _sized(cache[name], name, u, n_kv * capacity * n))
+    return c
+
+
+def validate_cache4(problem) -> int:
+    return lib().apb_validate_cache4(ctypes.byref(problem))
+
+
+def cache4_write(problem, k, v, cache: dict, stream=None):
+    """``apb_cache4_write``: quantise rows of ``k``/``v`` [n_kv, bf16_rows, d]
+    (bf16) into ``cache``, a mapping of ``k_codes``/``v_codes`` [n_kv, capacity,
+    d / 2] and ``k_scales``/``v_scales`` [n_kv, capacity, d / 32] (uint8)."""
+    p, b = problem, _bf16_types()
+    _check(validate_cache4(p), "apb_cache4_write")
+    n = p.n_kv_heads * p.bf16_rows * p.head_dim
+    st = lib().apb_cache4_write(
+        ctypes.byref(p), _sized(k, "k", b, n), _sized(v, "v", b, n),
+        ctypes.byref(_cache4(cache, p.n_kv_heads, p.capacity, p.head_dim)), _stream(stream))
+    _check(st, "apb_cache4_write")
+
+
+def cache4_read(problem, cache: dict, k, v, stream=None):
+    """``apb_cache4_read``: the values of cache rows into ``k``/``v`` [n_kv,
+    bf16_rows, d] (bf16); ``cache`` as in ``cache4_write``."""
+    p, b = problem, _bf16_types()
+    _check(validate_cache4(p), "apb_cache4_read")
+    n = p.n_kv_heads * p.bf16_rows * p.head_dim
+    st = lib().apb_cache4_read(
+        ctypes.byref(p), ctypes.byref(_cache4(cache, p.n_kv_heads, p.capacity, p.head_dim)),
+        _sized(k, "k", b, n), _sized(v, "v", b, n), _stream(stream))
+    _check(st, "apb_cache4_read")
+
+
+def validate_decode4(problem) -> int:
+    return lib().apb_validate_decode4(ctypes.byref(problem))
+
+
+def decode4_workspace_size(problem) -> int:
+    """``apb_decode4_workspace_size``: device scratch bytes a call needs."""
+    n = ctypes.c_uint64(0)
+    _check(lib().apb_decode4_workspace_size(ctypes.byref(problem), ctypes.byref(n)),
+           "apb_decode4_workspace_size")
+    return int(n.value)
+
+
+def decode4_attention(problem, q, cache: dict, o_part, lse_part, workspace, softmax_scale=0.0,
+                      stream=None):
+    """``apb_decode4_attention``: one host's stage-2 partial attention over a KV
+    cache in 4 bits (``cache`` as in ``cache4_write``; may be None when cache_len
+    is 0).  ``workspace`` is a device tensor of at least
+    ``decode4_workspace_size`` bytes (any dtype)."""
+    import torch
+    p, f = problem, (torch.float32,)
+    _check(validate_decode4(p), "apb_decode4_attention")
+    if workspace is None or not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous device tensor")
+    _on_current_device(workspace, "workspace")
+    rows, d = p.n_q_heads * p.n_new, p.head_dim
+    c = None if cache is None else ctypes.byref(_cache4(cache, p.n_kv_heads, p.capacity, d))
+    st = lib().apb_decode4_attention(
+        ctypes.byref(p), _sized(q, "q", _bf16_types(), rows * d), c,
+        _sized(o_part, "o_part", f, rows * d), _sized(lse_part, "lse_part", f, rows),
+        float(softmax_scale), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "apb_decode4_attention")

@@ -485,6 +485,164 @@ apb_status_t apb_decode_attention_noalloc(const apb_decode_problem_t* p, const u
   return APB_OK;
 }
 
+apb_status_t apb_validate_cache4(const apb_cache4_problem_t* p) {
+  if (!p) return APB_ERR_NULL_POINTER;
+  if (p->n_kv_heads < 1 || p->n_kv_heads > 65536 || p->head_dim < 1) return APB_ERR_BAD_SHAPE;
+  if (p->capacity < 1 || p->capacity > kMaxRows) return APB_ERR_BAD_SHAPE;
+  if (p->bf16_rows < 0 || p->bf16_rows > kMaxRows) return APB_ERR_BAD_SHAPE;
+  if (p->first_row < 0 || p->n_rows < 0 || p->bf16_first < 0) return APB_ERR_BAD_SHAPE;
+  if ((int64_t)p->first_row + p->n_rows > p->capacity) return APB_ERR_BAD_SHAPE;
+  if ((int64_t)p->bf16_first + p->n_rows > p->bf16_rows) return APB_ERR_BAD_SHAPE;
+  if (p->head_dim != 64 && p->head_dim != 128) return APB_ERR_UNSUPPORTED;
+  apb::Cache4Args a{};
+  a.n_kv = p->n_kv_heads; a.head_dim = p->head_dim; a.n_rows = p->n_rows;
+  if (apb::cache4_blocks(a) >= (int64_t(1) << 31)) return APB_ERR_BAD_SHAPE;
+  return APB_OK;
+}
+
+// Checks shared by the write and the read, and the kernel arguments of a valid
+// call; `moves` is whether there are rows to move.
+static apb_status_t cache4_checks(const apb_cache4_problem_t* p, const apb_cache4_t* cache,
+                                  const uint16_t* k, const uint16_t* v, bool write,
+                                  apb::Cache4Args* a, bool* moves) {
+  const apb_status_t st = apb_validate_cache4(p);
+  if (st != APB_OK) return st;
+  *moves = p->n_rows > 0;
+  if (!*moves) return APB_OK;
+  if (!cache || !k || !v) return APB_ERR_NULL_POINTER;
+  if (!cache->k_codes || !cache->k_scales || !cache->v_codes || !cache->v_scales)
+    return APB_ERR_NULL_POINTER;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(cache->k_codes, 16) ||
+      !aligned(cache->v_codes, 16) || !aligned(cache->k_scales, 4) || !aligned(cache->v_scales, 4))
+    return APB_ERR_MISALIGNED;
+  // whole tensors: all six lie apart, but that a write may take K and V from the
+  // same memory
+  const int64_t nkv = p->n_kv_heads, d = p->head_dim, cap = p->capacity;
+  const int64_t bytes = nkv * p->bf16_rows * d * 2;
+  const Range r[6] = {range_of(cache->k_codes, nkv * cap * (d / 2)),
+                      range_of(cache->k_scales, nkv * cap * (d / 32)),
+                      range_of(cache->v_codes, nkv * cap * (d / 2)),
+                      range_of(cache->v_scales, nkv * cap * (d / 32)),
+                      range_of(k, bytes), range_of(v, bytes)};
+  for (int i = 0; i < 6; ++i)
+    for (int j = i + 1; j < 6; ++j)
+      if (overlaps(r[i], r[j]) && !(write && i == 4)) return APB_ERR_ALIAS;
+  a->codes[0] = cache->k_codes; a->codes[1] = cache->v_codes;
+  a->scales[0] = cache->k_scales; a->scales[1] = cache->v_scales;
+  a->rows[0] = const_cast<uint16_t*>(k); a->rows[1] = const_cast<uint16_t*>(v);
+  a->n_kv = p->n_kv_heads; a->head_dim = p->head_dim; a->capacity = p->capacity;
+  a->first_row = p->first_row; a->n_rows = p->n_rows;
+  a->bf16_rows = p->bf16_rows; a->bf16_first = p->bf16_first;
+  return APB_OK;
+}
+
+apb_status_t apb_cache4_write(const apb_cache4_problem_t* p, const uint16_t* k, const uint16_t* v,
+                              const apb_cache4_t* cache, void* stream) {
+  apb::Cache4Args a{};
+  bool moves = false;
+  const apb_status_t st = cache4_checks(p, cache, k, v, true, &a, &moves);
+  if (st != APB_OK || !moves) return st;
+  const hipError_t e = apb::launch_cache4_write(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) {
+    set_last_error(e);
+    return APB_ERR_HIP;
+  }
+  return APB_OK;
+}
+
+apb_status_t apb_cache4_read(const apb_cache4_problem_t* p, const apb_cache4_t* cache, uint16_t* k,
+                             uint16_t* v, void* stream) {
+  apb::Cache4Args a{};
+  bool moves = false;
+  const apb_status_t st = cache4_checks(p, cache, k, v, false, &a, &moves);
+  if (st != APB_OK || !moves) return st;
+  const hipError_t e = apb::launch_cache4_read(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) {
+    set_last_error(e);
+    return APB_ERR_HIP;
+  }
+  return APB_OK;
+}
+
+apb_status_t apb_validate_decode4(const apb_decode4_problem_t* p) {
+  if (!p) return APB_ERR_NULL_POINTER;
+  if (p->n_kv_heads < 1 || p->n_kv_heads > 65536 || p->n_q_heads < 1 ||
+      p->n_q_heads % p->n_kv_heads != 0)
+    return APB_ERR_BAD_SHAPE;
+  if (p->head_dim < 1 || p->n_new < 1 || (p->causal != 0 && p->causal != 1))
+    return APB_ERR_BAD_SHAPE;
+  if (p->capacity < 1 || p->capacity > kMaxRows) return APB_ERR_BAD_SHAPE;
+  if (p->cache_len < 0 || p->cache_len > p->capacity) return APB_ERR_BAD_SHAPE;
+  if (p->causal == 1 && p->cache_len < p->n_new) return APB_ERR_BAD_SHAPE;
+  // rows of one GQA group and of the whole call stay well inside int32
+  if ((int64_t)p->n_q_heads * p->n_new > kMaxRows) return APB_ERR_BAD_SHAPE;
+  if (p->head_dim != 64 && p->head_dim != 128) return APB_ERR_UNSUPPORTED;
+  return APB_OK;
+}
+
+static apb::Decode4Args decode4_args(const apb_decode4_problem_t* p) {
+  apb::Decode4Args a{};
+  a.capacity = p->capacity; a.Lc = p->cache_len; a.n_new = p->n_new; a.causal = p->causal;
+  a.n_q = p->n_q_heads; a.n_kv = p->n_kv_heads; a.head_dim = p->head_dim;
+  return a;
+}
+
+apb_status_t apb_decode4_workspace_size(const apb_decode4_problem_t* p, uint64_t* bytes) {
+  const apb_status_t st = apb_validate_decode4(p);
+  if (st != APB_OK) return st;
+  if (!bytes) return APB_ERR_NULL_POINTER;
+  *bytes = apb::decode4_workspace_bytes(decode4_args(p));
+  return APB_OK;
+}
+
+apb_status_t apb_decode4_attention(const apb_decode4_problem_t* p, const uint16_t* q,
+                                   const apb_cache4_t* cache, float* o_part, float* lse_part,
+                                   float softmax_scale, void* workspace, uint64_t workspace_bytes,
+                                   void* stream) {
+  const apb_status_t st = apb_validate_decode4(p);
+  if (st != APB_OK) return st;
+  const bool has_cache = p->cache_len > 0;
+  if (!q || !o_part || !lse_part || !workspace) return APB_ERR_NULL_POINTER;
+  if (has_cache && (!cache || !cache->k_codes || !cache->k_scales || !cache->v_codes ||
+                    !cache->v_scales))
+    return APB_ERR_NULL_POINTER;
+  if (!aligned(q, 16) || !aligned(o_part, 16) || !aligned(lse_part, 4) || !aligned(workspace, 16))
+    return APB_ERR_MISALIGNED;
+  if (has_cache && (!aligned(cache->k_codes, 16) || !aligned(cache->v_codes, 16) ||
+                    !aligned(cache->k_scales, 4) || !aligned(cache->v_scales, 4)))
+    return APB_ERR_MISALIGNED;
+  apb::Decode4Args a = decode4_args(p);
+  const uint64_t need = apb::decode4_workspace_bytes(a);
+  if (workspace_bytes < need) return APB_ERR_BAD_SHAPE;
+  if (has_cache) {
+    a.k_codes = cache->k_codes; a.k_scales = cache->k_scales;
+    a.v_codes = cache->v_codes; a.v_scales = cache->v_scales;
+  }
+  const int64_t d = p->head_dim, rows = (int64_t)p->n_q_heads * p->n_new;
+  const int64_t cap = has_cache ? (int64_t)p->n_kv_heads * p->capacity : 0;
+  const Range in[5] = {range_of(q, rows * d * 2), range_of(a.k_codes, cap * (d / 2)),
+                       range_of(a.k_scales, cap * (d / 32)), range_of(a.v_codes, cap * (d / 2)),
+                       range_of(a.v_scales, cap * (d / 32))};
+  const Range out[3] = {range_of(o_part, rows * d * 4), range_of(lse_part, rows * 4),
+                        range_of(workspace, (int64_t)need)};
+  for (const Range& r : out)
+    for (const Range& i : in)
+      if (overlaps(r, i)) return APB_ERR_ALIAS;
+  if (overlaps(out[0], out[1]) || overlaps(out[0], out[2]) || overlaps(out[1], out[2]))
+    return APB_ERR_ALIAS;
+  float scale = softmax_scale;
+  if (!(scale > 0.f) || !isfinite(scale)) scale = 1.f / sqrtf((float)p->head_dim);
+  a.q = q; a.o = o_part; a.lse = lse_part;
+  a.workspace = static_cast<float*>(workspace);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const hipError_t e = apb::launch_decode4(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) {
+    set_last_error(e);
+    return APB_ERR_HIP;
+  }
+  return APB_OK;
+}
+
 apb_status_t apb_merge_partials(int32_t n_parts, int32_t rows, int32_t head_dim,
                                 const float* o_parts, const float* lse_parts, uint16_t* o,
                                 float* lse, void* stream) {

@@ -1,6 +1,6 @@
 // Internal launch interface between the C-ABI layer (apb_api.hip) and the
 // gfx950 kernels (apb_attention.hip, apb_compress.hip, apb_decode.hip,
-// apb_scorer.hip, apb_layer.hip).
+// apb_cache4.hip, apb_decode4.hip, apb_scorer.hip, apb_layer.hip).
 // Not installed.
 #ifndef APB_INTERNAL_H_
 #define APB_INTERNAL_H_
@@ -49,6 +49,30 @@ struct DecodeArgs {
   float* lse;          // [n_q][n_new]
   float* workspace;    // DecodePlan::workspace_bytes, 16-byte aligned
   int32_t Lc, n_new, append;
+  int32_t n_q, n_kv, head_dim;
+  float scale_log2;
+};
+
+// Rows between bf16 K/V and a cache in 4 bits, already validated; codes and
+// scales are K's and V's.
+struct Cache4Args {
+  uint8_t* codes[2];    // [n_kv][capacity][d / 2]
+  uint8_t* scales[2];   // [n_kv][capacity][d / 32]
+  uint16_t* rows[2];    // [n_kv][bf16_rows][d]: read by a write, written by a read
+  int32_t n_kv, head_dim, capacity, first_row, n_rows, bf16_rows, bf16_first;
+};
+
+// One host's decoding-stage attention over a cache in 4 bits, already validated.
+struct Decode4Args {
+  const uint16_t* q;         // [n_q][n_new][d]
+  const uint8_t* k_codes;    // [n_kv][capacity][d / 2]; null when Lc == 0
+  const uint8_t* k_scales;   // [n_kv][capacity][d / 32]
+  const uint8_t* v_codes;
+  const uint8_t* v_scales;
+  float* o;                  // [n_q][n_new][d]
+  float* lse;                // [n_q][n_new]
+  float* workspace;
+  int32_t capacity, Lc, n_new, causal;
   int32_t n_q, n_kv, head_dim;
   float scale_log2;
 };
@@ -112,6 +136,11 @@ hipError_t launch_decode(const DecodeArgs& a, const DecodePlan& pl, hipStream_t 
 constexpr uint64_t kDecodeScratchBytes = uint64_t(16) << 20;
 hipError_t decode_scratch(void** ptr);
 hipError_t launch_merge(const MergeArgs& a, hipStream_t stream);
+int64_t cache4_blocks(const Cache4Args& a);  // workgroups of a write or a read
+hipError_t launch_cache4_write(const Cache4Args& a, hipStream_t stream);
+hipError_t launch_cache4_read(const Cache4Args& a, hipStream_t stream);
+uint64_t decode4_workspace_bytes(const Decode4Args& a);
+hipError_t launch_decode4(const Decode4Args& a, hipStream_t stream);
 uint64_t scorer_workspace_bytes(const ScorerArgs& a);
 hipError_t launch_scorer(const ScorerArgs& a, hipStream_t stream);
 int scorer_hidden_block();  // hidden must be a multiple of this
