@@ -151,6 +151,34 @@ inline DecodePlan plan_decode(int64_t n_q, int64_t n_kv, int head_dim, int64_t c
   return pl;
 }
 
+// How a decode call over a 4-bit cache goes about it: 16 * rb rows of a KV head per
+// workgroup, whose four waves take the 32-key blocks of a split in turn.  The workspace
+// holds a partial per split and row: fp32 O, maximum and sum.
+struct Decode4Plan {
+  int n_split;
+  int blocks_per_split;
+  int rb;          // 16-row blocks of a workgroup (1, 2 or 4)
+  int row_blocks;  // workgroups along the rows of a KV head
+  uint64_t workspace_bytes;
+};
+
+inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t cache_len,
+                                int64_t n_new) {
+  Decode4Plan pl;
+  const int64_t R = n_q / n_kv * n_new, nblk = (cache_len + 31) / 32;
+  pl.rb = R <= 16 ? 1 : R <= 32 ? 2 : 4;
+  pl.row_blocks = (int)((R + 16 * pl.rb - 1) / (16 * pl.rb));
+  // two workgroups per CU, each wave with a block at least
+  int64_t n_split = std::min<int64_t>(2 * kCus / (n_kv * pl.row_blocks), (nblk + 3) / 4);
+  n_split = std::max<int64_t>(n_split, 1);
+  int64_t bps = std::max<int64_t>((nblk + n_split - 1) / n_split, 1);
+  n_split = std::max<int64_t>((nblk + bps - 1) / bps, 1);
+  pl.n_split = (int)n_split;
+  pl.blocks_per_split = (int)bps;
+  pl.workspace_bytes = (uint64_t)n_split * (uint64_t)(n_q * n_new) * (uint64_t)(head_dim + 2) * 4;
+  return pl;
+}
+
 // How the token tiles of one matrix product (apb_gemm.h) are cut: `full` tiles of
 // 256 tokens (nb = 8), then tiles of 32 * nb tokens for the rest.  The chip runs
 // one workgroup per CU, so a product takes whole rounds of 256 tiles, and one with
