@@ -413,30 +413,73 @@ def layer_fwd(problem, weights: dict, hidden_in, positions, k_cache, v_cache, pa
 # The elements that a call's sizes ask of each tensor are counted here: a cache
 # is sized by its capacity, not by the rows in use, so a tensor of another size
 # is an easy mistake, and one that the C call cannot see.  Nor can it see a tensor
-# of another device than the current one, whose stream the call would use.
-def _sized(t, name, dtypes, n):
-    ptr = _ptr(t, name, dtypes)
-    if t is not None:
-        if t.numel() != n:
-            raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
-        _on_current_device(t, name)
-    return ptr
+# of another device than the current one, whose stream the call would use.  A tensor
+# that is as it should be costs one expression (a call on a few rows takes 2 us of
+# the GPU, so what the host does is what it costs); what is wrong is found after.
+class _Call:
+    """The current device, the types and the stream of one call."""
+
+    __slots__ = ("where", "check", "problem", "dev")
+
+    def __init__(self, where, check, problem):
+        self.where, self.check, self.problem = where, check, problem
+        self.dev = _device()
+
+    def ptr(self, t, name, types, n):
+        if t is None:
+            return None
+        if (t.dtype in types and t.numel() == n and t.get_device() == self.dev
+                and t.is_contiguous()):
+            return t.data_ptr()
+        _check(self.check(self.problem), self.where)  # sizes that are wrong in themselves
+        _ptr(t, name, types)
+        if t.get_device() != self.dev:
+            raise ValueError(f"{name} is on {t.device}, not on the current device")
+        raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
+
+    def cache(self, c, n_kv, capacity, d):
+        codes, scales, u = n_kv * capacity * (d // 2), n_kv * capacity * (d // 32), _types().u8
+        return Cache4(self.ptr(c["k_codes"], "k_codes", u, codes),
+                      self.ptr(c["k_scales"], "k_scales", u, scales),
+                      self.ptr(c["v_codes"], "v_codes", u, codes),
+                      self.ptr(c["v_scales"], "v_scales", u, scales))
+
+    def stream(self, stream):
+        if stream is None and _types().raw_stream is not None:
+            return _types().raw_stream(self.dev)
+        return _stream(stream)
 
 
-def _on_current_device(t, name):
+class _Types:
+    def __init__(self):
+        import torch
+        self.bf16, self.f32, self.u8 = _bf16_types(), (torch.float32,), (torch.uint8,)
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.raw_device = getattr(torch._C, "_cuda_getDevice", None)
+        self.ready = False
+
+
+_known_types = None
+
+
+def _types():
+    global _known_types
+    if _known_types is None:
+        _known_types = _Types()
+    return _known_types
+
+
+def _device():
+    """The current device's index; -2 where there is none (no tensor's device)."""
+    t = _types()
+    if t.ready:
+        return t.raw_device()
     import torch
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
-
-
-def _cache4(cache, n_kv, capacity, d):
-    """``apb_cache4_t`` of a mapping of the four tensors (uint8)."""
-    import torch
-    u, c = (torch.uint8,), Cache4()
-    for name, n in (("k_codes", d // 2), ("k_scales", d // 32), ("v_codes", d // 2),
-                    ("v_scales", d // 32)):
-        setattr(c, name, _sized(cache[name], name, u, n_kv * capacity * n))
-    return c
+    if not torch.cuda.is_available():
+        return -2
+    dev = torch.cuda.current_device()  # initialises the runtime
+    t.ready = t.raw_device is not None
+    return dev
 
 
 def validate_cache4(problem) -> int:
@@ -447,25 +490,25 @@ def cache4_write(problem, k, v, cache: dict, stream=None):
     """``apb_cache4_write``: quantise rows of ``k``/``v`` [n_kv, bf16_rows, d]
     (bf16) into ``cache``, a mapping of ``k_codes``/``v_codes`` [n_kv, capacity,
     d / 2] and ``k_scales``/``v_scales`` [n_kv, capacity, d / 32] (uint8)."""
-    p, b = problem, _bf16_types()
-    _check(validate_cache4(p), "apb_cache4_write")
-    n = p.n_kv_heads * p.bf16_rows * p.head_dim
-    st = lib().apb_cache4_write(
-        ctypes.byref(p), _sized(k, "k", b, n), _sized(v, "v", b, n),
-        ctypes.byref(_cache4(cache, p.n_kv_heads, p.capacity, p.head_dim)), _stream(stream))
-    _check(st, "apb_cache4_write")
+    c, b = _Call("apb_cache4_write", validate_cache4, problem), _types().bf16
+    n_kv, d = problem.n_kv_heads, problem.head_dim
+    n = n_kv * problem.bf16_rows * d
+    st = lib().apb_cache4_write(problem, c.ptr(k, "k", b, n), c.ptr(v, "v", b, n),
+                                c.cache(cache, n_kv, problem.capacity, d), c.stream(stream))
+    if st:
+        _check(st, "apb_cache4_write")
 
 
 def cache4_read(problem, cache: dict, k, v, stream=None):
     """``apb_cache4_read``: the values of cache rows into ``k``/``v`` [n_kv,
     bf16_rows, d] (bf16); ``cache`` as in ``cache4_write``."""
-    p, b = problem, _bf16_types()
-    _check(validate_cache4(p), "apb_cache4_read")
-    n = p.n_kv_heads * p.bf16_rows * p.head_dim
-    st = lib().apb_cache4_read(
-        ctypes.byref(p), ctypes.byref(_cache4(cache, p.n_kv_heads, p.capacity, p.head_dim)),
-        _sized(k, "k", b, n), _sized(v, "v", b, n), _stream(stream))
-    _check(st, "apb_cache4_read")
+    c, b = _Call("apb_cache4_read", validate_cache4, problem), _types().bf16
+    n_kv, d = problem.n_kv_heads, problem.head_dim
+    n = n_kv * problem.bf16_rows * d
+    st = lib().apb_cache4_read(problem, c.cache(cache, n_kv, problem.capacity, d),
+                               c.ptr(k, "k", b, n), c.ptr(v, "v", b, n), c.stream(stream))
+    if st:
+        _check(st, "apb_cache4_read")
 
 
 def validate_decode4(problem) -> int:
@@ -486,17 +529,16 @@ def decode4_attention(problem, q, cache: dict, o_part, lse_part, workspace, soft
     cache in 4 bits (``cache`` as in ``cache4_write``; may be None when cache_len
     is 0).  ``workspace`` is a device tensor of at least
     ``decode4_workspace_size`` bytes (any dtype)."""
-    import torch
-    p, f = problem, (torch.float32,)
-    _check(validate_decode4(p), "apb_decode4_attention")
-    if workspace is None or not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous device tensor")
-    _on_current_device(workspace, "workspace")
-    rows, d = p.n_q_heads * p.n_new, p.head_dim
-    c = None if cache is None else ctypes.byref(_cache4(cache, p.n_kv_heads, p.capacity, d))
+    c, t = _Call("apb_decode4_attention", validate_decode4, problem), _types()
+    if workspace is None or workspace.get_device() != c.dev or not workspace.is_contiguous():
+        _check(validate_decode4(problem), "apb_decode4_attention")
+        raise ValueError("workspace must be a contiguous device tensor, on the current device")
+    rows, d = problem.n_q_heads * problem.n_new, problem.head_dim
     st = lib().apb_decode4_attention(
-        ctypes.byref(p), _sized(q, "q", _bf16_types(), rows * d), c,
-        _sized(o_part, "o_part", f, rows * d), _sized(lse_part, "lse_part", f, rows),
-        float(softmax_scale), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream(stream))
-    _check(st, "apb_decode4_attention")
+        problem, c.ptr(q, "q", t.bf16, rows * d),
+        None if cache is None else c.cache(cache, problem.n_kv_heads, problem.capacity, d),
+        c.ptr(o_part, "o_part", t.f32, rows * d), c.ptr(lse_part, "lse_part", t.f32, rows),
+        softmax_scale, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        c.stream(stream))
+    if st:
+        _check(st, "apb_decode4_attention")
