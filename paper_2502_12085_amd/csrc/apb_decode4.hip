@@ -56,7 +56,7 @@ struct Dec4Params {
   float* part_l;    // [n_split][rows_total]: sum against it
   float* o;         // one split: the result
   float* lse;
-  int capacity, Lc, n_new, causal, R, rows_total, n_split, n_rb, blocks_per_split;
+  int capacity, Lc, n_new, causal, n_kv, R, rows_total, n_split, n_rb, blocks_per_split;
   float scale_log2;
 };
 
@@ -91,164 +91,104 @@ __device__ __forceinline__ int v_swz(int r) { return D == 128 ? 2 * (r & 7) : 2 
 template <int D>
 __device__ __forceinline__ int v_flip(int r) { return D == 128 ? (r >> 1) & 1 : (r >> 2) & 1; }
 
+// K, for reads of a chunk of 16 rows at once.
+template <int D>
+__device__ __forceinline__ int k_swz(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+
+// A lane's first transposing read of a V tile: rows 4 lg .. 4 lg + 3 of dims 0 .. 15
+// between the 16 lanes of a group (dim block db is 32 db away by exclusive or, rows 16 on
+// 16 rows); the lane then has element li of its group's four rows.
+template <int D>
+__device__ __forceinline__ uint32_t v_lane(int li, int lg) {
+  const int row = 4 * lg + (li >> 2);
+  return (uint32_t)(row * 2 * D + 16 * (((li & 3) >> 1) ^ v_swz<D>(row)) + 8 * (li & 1));
+}
+
+// 32 values of one key into its row's four chunks; a group of NaN as zeros.
+__device__ __forceinline__ void put_values(uint32_t at, u32x4 codes, unsigned b, bool flip) {
+  const bool bad = b == 255;
+  const float scale = __uint_as_float(bad ? 0u : b << 23);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const unsigned there = codes[j ^ 1], here = codes[j];
+    *(lds_u32x4*)(uintptr_t)(at ^ (16u * j)) = elements(bad ? 0u : flip ? there : here, scale);
+  }
+}
+
 __device__ __forceinline__ float across_groups_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
-// Workgroup: split (fastest), row block, KV head.
-template <int D, int RB, int WK, bool WHOLE>
-__global__ void __launch_bounds__(64 * WK, RB == 4 ? 1 : 2) decode4_kernel(Dec4Params p) {
-  constexpr int NDB = D / 16, KW = Block4<D>::KW, VL = Block4<D>::VL;
-  constexpr int TILE = 32 * D * 2;            // bytes of a V tile
-  constexpr int OUT = RB * NDB * 4 * 64 * 4;  // bytes of a wave's O
-  constexpr int LDS = WK * (OUT > TILE && WK > 1 ? OUT : TILE);
-  __shared__ __attribute__((aligned(256))) uint8_t lds[LDS];
-  __shared__ float ml_lds[2][WK][RB][16];
+// Where workgroup `id` works.  Its XCD is id % 8: the row blocks of one split of one KV
+// head, which read the same keys, go to one XCD and so to one L2.
+struct Place4 {
+  int split, row_block, kvh;
+};
 
-  const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
-  const int wave = WK == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int split = blockIdx.x % p.n_split;
-  const int rb0 = (int)(blockIdx.x / p.n_split) % p.n_rb * RB;
-  const int kvh = (int)(blockIdx.x / p.n_split) / p.n_rb;
-  const int nblk = (p.Lc + 31) / 32;
-  const int b0 = split * p.blocks_per_split, b1 = min(b0 + p.blocks_per_split, nblk);
+__device__ __forceinline__ Place4 place4(int n_split, int n_rb, int n_kv) {
+  const unsigned id = blockIdx.x, pairs = (unsigned)n_split * n_kv, full = pairs / 8 * 8 * n_rb;
+  unsigned rb, u;
+  if (id < full) {
+    rb = id % (8 * n_rb) / 8;
+    u = id / (8 * n_rb) * 8 + id % 8;
+  } else {
+    const unsigned rest = pairs % 8;
+    rb = (id - full) / rest;
+    u = pairs / 8 * 8 + (id - full) % rest;
+  }
+  return Place4{(int)(u % n_split), (int)rb, (int)(u / n_split)};
+}
 
-  // This lane's rows (MFMA column li of every row block) and the keys they see.
-  int vis[RB];
+// A wave's state: 16 * RB rows, row li of each block in the four lanes li + 16 lg.
+template <int D, int RB>
+struct Rows4 {
+  static constexpr int NDB = D / 16, KW = D / 32;
+  int vis[RB];            // keys that the lane's rows see
   bf16x8 q[RB][KW];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int rho = (rb0 + rb) * 16 + li;
-    const bool ok = rho < p.R;
-    vis[rb] = p.causal ? p.Lc - p.n_new + (ok ? rho % p.n_new : 0) + 1 : p.Lc;
-    const uint16_t* row = p.q + ((size_t)kvh * p.R + (ok ? rho : 0)) * D + lg * (D / 4);
-#pragma unroll
-    for (int j = 0; j < KW; ++j)
-      q[rb][j] = as_bf16(*reinterpret_cast<const u32x4*>(row + 8 * j) & (ok ? ~0u : 0u));
-  }
-  const int vis_all = p.causal ? p.Lc - p.n_new + 1 : p.Lc;  // keys that every row sees
-
-  // V: lane -> (key, group) of each 16-byte load, and its place in the tile.
-  constexpr int G = D / 32;
-  const uint32_t tile = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds +
-                        (uint32_t)(wave * TILE);
-  uint32_t v_put[VL];
-#pragma unroll
-  for (int v = 0; v < VL; ++v) {
-    const int key = (64 * v + lane) / G, g = lane % G;
-    v_put[v] = tile + (uint32_t)(key * 2 * D + 16 * ((4 * g) ^ v_swz<D>(key) ^ v_flip<D>(key)));
-  }
-  const bool flip = v_flip<D>(lane / G) != 0;  // (the same for every v: 64 / G keys apart)
-  uint32_t v_get;
-  {
-    const int row = 4 * lg + (li >> 2);
-    v_get = tile + (uint32_t)(row * 2 * D + 16 * (((li & 3) >> 1) ^ v_swz<D>(row)) + 8 * (li & 1));
-  }
-
-  auto load = [&](int b) __attribute__((always_inline)) {
-    Block4<D> x;
-    const int c0 = 32 * b, last = p.Lc - 1 - c0;  // rows past the last key repeat it
-    const size_t r0 = (size_t)kvh * p.capacity + c0;
-    const uint8_t* kc = p.k_codes + r0 * (D / 2);
-    const uint8_t* ks = p.k_scales + r0 * G;
-    const uint8_t* vc = p.v_codes + r0 * (D / 2);
-    const uint8_t* vs = p.v_scales + r0 * G;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t key = (uint32_t)min(16 * i + li, last);
-      if constexpr (D == 128) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(kc + (key * (D / 2) + 16u * lg));
-        x.kw[i][0] = w[0]; x.kw[i][1] = w[1]; x.kw[i][2] = w[2]; x.kw[i][3] = w[3];
-        x.kb[i] = ks[key * G + lg];
-      } else {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(kc + (key * (D / 2) + 8u * lg));
-        x.kw[i][0] = w[0]; x.kw[i][1] = w[1];
-        x.kb[i] = ks[key * G + lg / 2];
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < VL; ++v) {
-      const uint32_t key = (uint32_t)min((64 * v + lane) / G, last), g = lane % G;
-      x.vw[v] = *reinterpret_cast<const u32x4*>(vc + (key * (D / 2) + 16u * g));
-      x.vb[v] = vs[key * G + g];
-    }
-    return x;
-  };
-
-  f32x4 oacc[RB][NDB];
+  f32x4 oacc[RB][NDB];    // element r of dim block db: O^T[16 db + 4 lg + r][row li]
   float m_run[RB], l_run[RB];
+
+  // Rows from row0 on of KV head kvh; q's dims of product j from dim(j) on.
+  template <typename Dim>
+  __device__ __forceinline__ void start(const Dec4Params& p, int kvh, int row0, Dim dim) {
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    m_run[rb] = -INFINITY;
-    l_run[rb] = 0.f;
+    for (int rb = 0; rb < RB; ++rb) {
+      const int rho = row0 + 16 * rb + (threadIdx.x & 15);
+      const bool ok = rho < p.R;
+      vis[rb] = p.causal ? p.Lc - p.n_new + (ok ? rho % p.n_new : 0) + 1 : p.Lc;
+      const uint16_t* row = p.q + ((size_t)kvh * p.R + (ok ? rho : 0)) * D;
 #pragma unroll
-    for (int db = 0; db < NDB; ++db) oacc[rb][db] = f32x4{};
+      for (int j = 0; j < KW; ++j)
+        q[rb][j] = as_bf16(*reinterpret_cast<const u32x4*>(row + dim(j)) & (ok ? ~0u : 0u));
+      m_run[rb] = -INFINITY;
+      l_run[rb] = 0.f;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) oacc[rb][db] = f32x4{};
+    }
   }
 
-  Block4<D> next;
-  if (b0 + wave < b1) next = load(b0 + wave);
-  for (int b = b0 + wave; b < b1; b += WK) {
-    const Block4<D> x = next;
-    if (b + WK < b1) next = load(b + WK);
-    const int c0 = 32 * b;
+  // Keys that the rows do not see, of the 32 from c0 on.
+  __device__ __forceinline__ void mask(f32x4 (&s)[2][RB], int c0, int lg) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (c0 + 16 * i + 4 * lg + r >= vis[rb]) s[i][rb][r] = -INFINITY;
+  }
 
-    // S^T: element r of tile i of this lane is key c0 + 16 i + 4 lg + r
-    f32x4 s[2][RB];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float scale = __uint_as_float(x.kb[i] << 23);  // b = 255: NaN elements
-#pragma unroll
-      for (int j = 0; j < KW; ++j) {
-        const bf16x8 k = as_bf16(elements(x.kw[i][j], scale));
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          const f32x4 zero = {};
-          s[i][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[rb][j], j == 0 ? zero : s[i][rb],
-                                                             0, 0, 0);
-        }
-      }
-    }
-
-    // V -> LDS.  A group of NaN goes there as zeros, and into O by hand, for the
-    // rows that see it: in a product a zero probability would not keep it out.
-    bool bad = false;
-#pragma unroll
-    for (int v = 0; v < VL; ++v) bad |= x.vb[v] == 255;
-    const bool any_bad = __any(bad);
-#pragma unroll
-    for (int v = 0; v < VL; ++v) {
-      unsigned w[4] = {x.vw[v][0], x.vw[v][1], x.vw[v][2], x.vw[v][3]};
-      float scale = __uint_as_float(x.vb[v] << 23);
-      if (any_bad && x.vb[v] == 255) {
-        w[0] = w[1] = w[2] = w[3] = 0;
-        scale = 1.f;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const unsigned mine = flip ? w[j ^ 1] : w[j];
-        *(lds_u32x4*)(uintptr_t)(v_put[v] ^ (16u * j)) = elements(mine, scale);
-      }
-    }
-
-    if (c0 + 32 > vis_all) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (c0 + 16 * i + 4 * lg + r >= vis[rb]) s[i][rb][r] = -INFINITY;
-    }
-
-    u32x4 pr[RB][3];  // the probabilities' three parts, as the P operand
+  // Logits (element r of tile i: key 16 i + 4 lg + r) to probabilities, in their three
+  // parts as the P operand, and the running maximum and sum.
+  __device__ __forceinline__ void softmax(const f32x4 (&s)[2][RB], float scale, u32x4 (&pr)[RB][3]) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       float e[8], sum;
       auto exps = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          e[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][rb][i & 3], p.scale_log2, -m_run[rb]));
+          e[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][rb][i & 3], scale, -m_run[rb]));
         sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       };
       exps();
@@ -256,7 +196,7 @@ __global__ void __launch_bounds__(64 * WK, RB == 4 ? 1 : 2) decode4_kernel(Dec4P
         float mx = s[0][rb][0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i >> 2][rb][i & 3]);
-        const float m_new = fmaxf(m_run[rb], across_groups_max(mx) * p.scale_log2);
+        const float m_new = fmaxf(m_run[rb], across_groups_max(mx) * scale);
         if (m_new == -INFINITY) {
           // nothing but keys that the row does not see, and NaN, which stays
           sum = 0.f;
@@ -291,8 +231,10 @@ __global__ void __launch_bounds__(64 * WK, RB == 4 ? 1 : 2) decode4_kernel(Dec4P
         pr[rb][2][i] = __builtin_amdgcn_perm(lo[1], lo[0], 0x07060302u);
       }
     }
+  }
 
-    // O^T += V^T P^T
+  // O^T += V^T P^T over a tile of 32 rows of V in LDS; v_get: the lane's first address.
+  __device__ __forceinline__ void values(uint32_t v_get, const u32x4 (&pr)[RB][3]) {
 #pragma unroll
     for (int db = 0; db < NDB; ++db) {
       i16x4 part[2];
@@ -309,6 +251,180 @@ __global__ void __launch_bounds__(64 * WK, RB == 4 ? 1 : 2) decode4_kernel(Dec4P
           oacc[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, as_bf16(pr[rb][t]), oacc[rb][db],
                                                                  0, 0, 0);
     }
+  }
+
+  // Values of group g (dims 32 g ..) of key c are NaN: so is O of the rows that see it.
+  __device__ __forceinline__ void not_a_number(int g, int c) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+        if (db / 2 == g && c < vis[rb]) oacc[rb][db] = f32x4{} + NAN;
+  }
+
+  // The parts of WK waves over the same rows (this one the wk-th) meet in LDS at o_lds, 16
+  // bytes a lane for each dim block and wave, and ml_lds; then dim block db goes out from
+  // wave db % WK.
+  template <int WK, bool WHOLE>
+  __device__ __forceinline__ void finish(const Dec4Params& p, const Place4& at, int row0, int wk,
+                                         uint8_t* o_lds, float (*ml_lds)[WK][RB][16]) {
+    constexpr int OUT = RB * NDB * 4 * 64 * 4;  // bytes of a wave's O
+    const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {  // sums over the four lanes of a row
+      l_run[rb] += __shfl_xor(l_run[rb], 16);
+      l_run[rb] += __shfl_xor(l_run[rb], 32);
+    }
+    __syncthreads();  // the tiles are done with
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+        *reinterpret_cast<f32x4*>(o_lds + wk * OUT + 1024 * (rb * NDB + db) + 16 * lane) = oacc[rb][db];
+      if (lg == 0) {
+        ml_lds[0][wk][rb][li] = m_run[rb];
+        ml_lds[1][wk][rb][li] = l_run[rb];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int rho = row0 + 16 * rb + li;
+      if (rho >= p.R) continue;
+      float m = -INFINITY, l = 0.f, w[WK];
+#pragma unroll
+      for (int k = 0; k < WK; ++k) m = fmaxf(m, ml_lds[0][k][rb][li]);
+#pragma unroll
+      for (int k = 0; k < WK; ++k) {
+        const float lk = ml_lds[1][k][rb][li];  // (0: no key; NaN stays)
+        w[k] = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml_lds[0][k][rb][li] - m);
+        l = fmaf(w[k], lk, l);
+      }
+      const size_t row = (size_t)at.kvh * p.R + rho;
+      const float inv = !WHOLE ? 1.f : l == 0.f ? 0.f : 1.f / l;
+      float* out = (WHOLE ? p.o : p.part_o + (size_t)at.split * p.rows_total * D) + row * D + 4 * lg;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        if (db % WK != wk) continue;
+        f32x4 y = {};
+#pragma unroll
+        for (int k = 0; k < WK; ++k)
+          y += w[k] *
+               *reinterpret_cast<const f32x4*>(o_lds + k * OUT + 1024 * (rb * NDB + db) + 16 * lane);
+        *reinterpret_cast<f32x4*>(out + 16 * db) = y * inv;
+      }
+      if (wk == 0 && lg == 0) {
+        if constexpr (WHOLE) {
+          p.lse[row] = l == 0.f ? -INFINITY : 0.69314718055994531f * (m + log2f(l));
+        } else {
+          p.part_m[(size_t)at.split * p.rows_total + row] = m;
+          p.part_l[(size_t)at.split * p.rows_total + row] = l;
+        }
+      }
+    }
+  }
+};
+
+// Up to 32 rows of a KV head: WK waves, each with 32-key blocks of its own.
+template <int D, int RB, int WK, bool WHOLE>
+__global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
+  using Rows = Rows4<D, RB>;
+  constexpr int KW = Block4<D>::KW, VL = Block4<D>::VL;
+  constexpr int TILE = 32 * D * 2, OUT = RB * D * 64;  // bytes of a V tile, of a wave's O
+  __shared__ __attribute__((aligned(256))) uint8_t lds[WK * (OUT > TILE ? OUT : TILE)];
+  __shared__ float ml_lds[2][WK][RB][16];
+
+  const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Place4 at = place4(p.n_split, p.n_rb, p.n_kv);
+  const int nblk = (p.Lc + 31) / 32;
+  const int b0 = at.split * p.blocks_per_split, b1 = min(b0 + p.blocks_per_split, nblk);
+  const int vis_all = p.causal ? p.Lc - p.n_new + 1 : p.Lc;  // keys that every row sees
+
+  // V: lane -> (key, group) of each 16-byte load, and its place in the tile.
+  constexpr int G = D / 32;
+  const uint32_t tile = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds +
+                        (uint32_t)(wave * TILE);
+  uint32_t v_put[VL];
+#pragma unroll
+  for (int v = 0; v < VL; ++v) {
+    const int key = (64 * v + lane) / G, g = lane % G;
+    v_put[v] = tile + (uint32_t)(key * 2 * D + 16 * ((4 * g) ^ v_swz<D>(key) ^ v_flip<D>(key)));
+  }
+  const bool flip = v_flip<D>(lane / G) != 0;  // (the same for every v: 64 / G keys apart)
+  const uint32_t v_get = tile + v_lane<D>(li, lg);
+
+  auto load = [&](int b) __attribute__((always_inline)) {
+    Block4<D> x;
+    const int c0 = 32 * b, last = p.Lc - 1 - c0;  // rows past the last key repeat it
+    const size_t r0 = (size_t)at.kvh * p.capacity + c0;
+    const uint8_t* kc = p.k_codes + r0 * (D / 2);
+    const uint8_t* ks = p.k_scales + r0 * G;
+    const uint8_t* vc = p.v_codes + r0 * (D / 2);
+    const uint8_t* vs = p.v_scales + r0 * G;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t key = (uint32_t)min(16 * i + li, last);
+      if constexpr (D == 128) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(kc + (key * (D / 2) + 16u * lg));
+        x.kw[i][0] = w[0]; x.kw[i][1] = w[1]; x.kw[i][2] = w[2]; x.kw[i][3] = w[3];
+        x.kb[i] = ks[key * G + lg];
+      } else {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(kc + (key * (D / 2) + 8u * lg));
+        x.kw[i][0] = w[0]; x.kw[i][1] = w[1];
+        x.kb[i] = ks[key * G + lg / 2];
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < VL; ++v) {
+      const uint32_t key = (uint32_t)min((64 * v + lane) / G, last), g = lane % G;
+      x.vw[v] = *reinterpret_cast<const u32x4*>(vc + (key * (D / 2) + 16u * g));
+      x.vb[v] = vs[key * G + g];
+    }
+    return x;
+  };
+
+  Rows rows;
+  const int row0 = 16 * RB * at.row_block;
+  // (a lane's d / 4 elements of its key lie together)
+  rows.start(p, at.kvh, row0, [&](int j) { return lg * (D / 4) + 8 * j; });
+
+  Block4<D> next;
+  if (b0 + wave < b1) next = load(b0 + wave);
+  for (int b = b0 + wave; b < b1; b += WK) {
+    const Block4<D> x = next;
+    if (b + WK < b1) next = load(b + WK);
+    const int c0 = 32 * b;
+
+    f32x4 s[2][RB];  // S^T: element r of tile i is key c0 + 16 i + 4 lg + r
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float scale = __uint_as_float(x.kb[i] << 23);  // b = 255: NaN elements
+#pragma unroll
+      for (int j = 0; j < KW; ++j) {
+        const bf16x8 k = as_bf16(elements(x.kw[i][j], scale));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          const f32x4 zero = {};
+          s[i][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[rb][j],
+                                                             j == 0 ? zero : s[i][rb], 0, 0, 0);
+        }
+      }
+    }
+
+    // V -> LDS.  A group of NaN goes there as zeros, and into O by hand, for the
+    // rows that see it: in a product a zero probability would not keep it out.
+    bool bad = false;
+#pragma unroll
+    for (int v = 0; v < VL; ++v) bad |= x.vb[v] == 255;
+    const bool any_bad = __any(bad);
+#pragma unroll
+    for (int v = 0; v < VL; ++v) put_values(v_put[v], x.vw[v], x.vb[v], flip);
+
+    if (c0 + 32 > vis_all) rows.mask(s, c0, lg);
+    u32x4 pr[RB][3];
+    rows.softmax(s, p.scale_log2, pr);
+    rows.values(v_get, pr);
 
     if (any_bad) {  // the first key of each group's NaN
 #pragma unroll
@@ -319,149 +435,227 @@ __global__ void __launch_bounds__(64 * WK, RB == 4 ? 1 : 2) decode4_kernel(Dec4P
           const unsigned long long hit = __ballot(x.vb[v] == 255 && (int)(lane % G) == g);
           if (hit) first = min(first, (64 * v + (int)__builtin_ctzll(hit)) / G);
         }
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-          if (first < 32 && c0 + first < vis[rb])
-            oacc[rb][2 * g] = oacc[rb][2 * g + 1] = f32x4{} + NAN;
+        if (first < 32) rows.not_a_number(g, c0 + first);
       }
     }
   }
+  rows.template finish<WK, WHOLE>(p, at, row0, wave, lds, ml_lds);
+}
 
-  // sums over the four lanes of a row
+// More rows: eight waves, WR of them with 32 rows each and WK = 8 / WR such sets, which
+// take a split's keys in turn.  A step is 128 keys: all threads make its codes bf16
+// and put K and V into LDS, where each set reads 128 / WK of them, so that the work of a
+// conversion is shared by 32 * WR rows.  The next step's codes are in flight and its
+// conversion is among this one's products; two buffers, one barrier a step.
+template <int D, int WR, bool WHOLE>
+__global__ void __launch_bounds__(512, 2) decode4_shared_kernel(Dec4Params p) {
+  constexpr int RB = 2, WK = 8 / WR, SUB = 4 / WK;  // 32-key blocks of a step and set
+  using Rows = Rows4<D, RB>;
+  constexpr int KW = D / 32, G = D / 32, TILE = 32 * D * 2;
+  constexpr int UNITS = 128 * G / 512 > 0 ? 1 : 0;  // of K and of V in each thread, or K or V
+  static_assert(UNITS == (D == 128), "a thread's share of a step");
+  __shared__ __attribute__((aligned(256))) uint8_t lds[2][2][4][TILE];  // buffer, K or V, block
+  __shared__ float ml_lds[WR][2][WK][RB][16];
+  // First key (of 32) whose values of a group are NaN, and whether there is one, by step % 3:
+  // cleared in the step before it is set.
+  __shared__ int nan_lds[3][4][4], any_lds[3];
+
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
+  const Place4 at = place4(p.n_split, p.n_rb, p.n_kv);
+  const int nblk = (p.Lc + 31) / 32;
+  const int b0 = at.split * p.blocks_per_split, b1 = min(b0 + p.blocks_per_split, nblk);
+  const int steps = (b1 - b0 + 3) / 4;
+  const int vis_all = p.causal ? p.Lc - p.n_new + 1 : p.Lc;
+
+  // This thread's groups of a step: (key, g) of K and of V (d = 128), or of one of them.
+  const int unit = D == 128 ? tid : tid & 255, key = unit / G, g = unit % G;
+  const bool has_k = D == 128 || tid < 256, has_v = D == 128 || tid >= 256;
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+  const uint32_t row = (uint32_t)(key * 2 * D);  // (blocks follow one another)
+  const uint32_t k_put = base + row + 16u * ((4 * g) ^ k_swz<D>(key));
+  const uint32_t v_put = base + 4 * TILE + row + 16u * ((4 * g) ^ v_swz<D>(key) ^ v_flip<D>(key));
+  const bool flip = v_flip<D>(key) != 0;
+  constexpr uint32_t BUF = 8 * TILE;
+
+  u32x4 kw = {}, vw = {};
+  unsigned kb = 0, vb = 0;
+  auto load = [&](int step) __attribute__((always_inline)) {
+    const int c0 = 32 * (b0 + 4 * step);
+    const uint32_t k = (uint32_t)min(key, p.Lc - 1 - c0);  // rows past the last key repeat it
+    const size_t r0 = (size_t)at.kvh * p.capacity + c0;
+    if (has_k) {
+      kw = *reinterpret_cast<const u32x4*>(p.k_codes + r0 * (D / 2) + (k * (D / 2) + 16u * g));
+      kb = (p.k_scales + r0 * G)[k * G + g];
+    }
+    if (has_v) {
+      vw = *reinterpret_cast<const u32x4*>(p.v_codes + r0 * (D / 2) + (k * (D / 2) + 16u * g));
+      vb = (p.v_scales + r0 * G)[k * G + g];
+    }
+  };
+  auto put = [&](int step) __attribute__((always_inline)) {
+    const uint32_t buf = step & 1 ? BUF : 0;
+    if (has_k) {
+      const float scale = __uint_as_float(kb << 23);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    l_run[rb] += __shfl_xor(l_run[rb], 16);
-    l_run[rb] += __shfl_xor(l_run[rb], 32);
+      for (int j = 0; j < 4; ++j)
+        *(lds_u32x4*)(uintptr_t)((k_put + buf) ^ (16u * j)) = elements(kw[j], scale);
+    }
+    if (has_v) {
+      put_values(v_put + buf, vw, vb, flip);
+      if (vb == 255) {
+        atomicMin(&nan_lds[step % 3][key / 32][g], key % 32);
+        any_lds[step % 3] = 1;
+      }
+    }
+  };
+  auto clear = [&](int step) __attribute__((always_inline)) {
+    if (tid < 16) nan_lds[step % 3][tid / 4][tid % 4] = 32;
+    if (tid == 16) any_lds[step % 3] = 0;
+  };
+
+  Rows rows;
+  const int row0 = 32 * (WR * at.row_block + wr);
+  const bool has_rows = row0 < p.R;
+  rows.start(p, at.kvh, row0, [&](int j) { return 32 * j + 8 * lg; });
+  const uint32_t v_get = base + 4 * TILE + v_lane<D>(li, lg);
+  const uint32_t k_get = base + (uint32_t)(li * 2 * D) + 16u * (lg ^ k_swz<D>(li));
+
+  if (steps > 0) {
+    load(0);
+    clear(0);
+    clear(1);
+    __syncthreads();
+    put(0);
+    if (steps > 1) load(1);
   }
-  // the waves' parts: O, maximum and sum through LDS, then dim block db to wave db % WK
-  float w[RB][WK], m_all[RB], l_all[RB];
-  float* const mine = reinterpret_cast<float*>(lds + (WK > 1 ? wave * OUT : 0)) + 4 * lane;
-  if constexpr (WK > 1) {
-    __syncthreads();  // the tiles are done with (a wave's O may lie over another's)
+  __syncthreads();
+  for (int step = 0; step < steps; ++step) {
+    if (step + 1 < steps) {
+      put(step + 1);
+      if (step + 2 < steps) load(step + 2);
+    }
+    clear(step + 2);
+    const bool any_bad = any_lds[step % 3] != 0;
+    const uint32_t buf = step & 1 ? BUF : 0;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
+    for (int t = 0; t < SUB; ++t) {
+      const int blk = wk * SUB + t, b = b0 + 4 * step + blk, c0 = 32 * b;
+      if (b >= b1 || !has_rows) continue;
+      const uint32_t kt = k_get + buf + blk * TILE;
+      f32x4 s[2][RB];
 #pragma unroll
-      for (int db = 0; db < NDB; ++db)
-        *reinterpret_cast<f32x4*>(mine + 256 * (rb * NDB + db)) = oacc[rb][db];
-      if (lg == 0) {
-        ml_lds[0][wave][rb][li] = m_run[rb];
-        ml_lds[1][wave][rb][li] = l_run[rb];
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < KW; ++j) {
+          const bf16x8 k = as_bf16(*(lds_u32x4*)(uintptr_t)((kt ^ (64u * j)) + (uint32_t)(16 * i * 2 * D)));
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
+            const f32x4 zero = {};
+            s[i][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[rb][j],
+                                                               j == 0 ? zero : s[i][rb], 0, 0, 0);
+          }
+        }
+      if (c0 + 32 > vis_all) rows.mask(s, c0, lg);
+      u32x4 pr[RB][3];
+      rows.softmax(s, p.scale_log2, pr);
+      rows.values(v_get + buf + blk * TILE, pr);
+      if (any_bad) {
+        for (int n = 0; n < G; ++n) {
+          const int first = nan_lds[step % 3][blk][n];
+          if (first < 32) rows.not_a_number(n, c0 + first);
+        }
       }
     }
     __syncthreads();
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      m_all[rb] = -INFINITY;
-      l_all[rb] = 0.f;
-#pragma unroll
-      for (int k = 0; k < WK; ++k) m_all[rb] = fmaxf(m_all[rb], ml_lds[0][k][rb][li]);
-#pragma unroll
-      for (int k = 0; k < WK; ++k) {
-        const float l = ml_lds[1][k][rb][li];  // (0: no key; NaN stays)
-        w[rb][k] = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml_lds[0][k][rb][li] - m_all[rb]);
-        l_all[rb] = fmaf(w[rb][k], l, l_all[rb]);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      m_all[rb] = m_run[rb];
-      l_all[rb] = l_run[rb];
-    }
   }
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int rho = (rb0 + rb) * 16 + li;
-    if (rho >= p.R) continue;
-    const size_t row = (size_t)kvh * p.R + rho;
-    const float inv = !WHOLE ? 1.f : l_all[rb] == 0.f ? 0.f : 1.f / l_all[rb];
-    float* out = (WHOLE ? p.o : p.part_o + (size_t)split * p.rows_total * D) + row * D + 4 * lg;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-      if (WK > 1 && db % WK != wave) continue;
-      f32x4 y = {};
-      if constexpr (WK > 1) {
-#pragma unroll
-        for (int k = 0; k < WK; ++k)
-          y += w[rb][k] * *reinterpret_cast<const f32x4*>(
-                              reinterpret_cast<float*>(lds + k * OUT) + 4 * lane + 256 * (rb * NDB + db));
-      } else {
-        y = oacc[rb][db];
-      }
-      *reinterpret_cast<f32x4*>(out + 16 * db) = y * inv;
-    }
-    if (wave == 0 && lg == 0) {
-      if constexpr (WHOLE) {
-        p.lse[row] = l_all[rb] == 0.f ? -INFINITY
-                                      : 0.69314718055994531f * (m_all[rb] + log2f(l_all[rb]));
-      } else {
-        p.part_m[(size_t)split * p.rows_total + row] = m_all[rb];
-        p.part_l[(size_t)split * p.rows_total + row] = l_all[rb];
-      }
-    }
-  }
+  rows.template finish<WK, WHOLE>(p, at, row0, wk, &lds[0][0][0][0] + wr * WK * RB * D * 64, ml_lds[wr]);
 }
 
 // The splits of a row: O = sum_s 2^(m_s - m) O_s / l, l = sum_s 2^(m_s - m) l_s, with m
 // the largest m_s; lse = ln 2 (m + log2 l).  Parts keep O undivided, and m apart from
 // log l: a sum of the two would lose l's digits beside a large m.  A workgroup per row,
-// 16 bytes a thread, thread groups taking every G-th split.
+// 16 bytes of O a thread; a thread takes every G-th split, eight at a time against its
+// own maximum, so that all it reads is one trip to memory, and the thread groups meet in
+// LDS.
 constexpr int kMergeThreads = 256;
 
 template <int D>
 __global__ void __launch_bounds__(kMergeThreads) decode4_merge_kernel(
     int n_split, int rows, const float* __restrict__ part_o, const float* __restrict__ part_m,
     const float* __restrict__ part_l, float* __restrict__ o, float* __restrict__ lse) {
-  constexpr int TPR = D / 4, G = kMergeThreads / TPR;
+  constexpr int TPR = D / 4, G = kMergeThreads / TPR, U = 8;
   __shared__ f32x4 acc_lds[kMergeThreads];
-  __shared__ float red[kMergeThreads / 64], l_lds[G];
+  __shared__ float m_lds[G], l_lds[G];
   const int tid = threadIdx.x, row = blockIdx.x, grp = tid / TPR, c = tid % TPR;
-  float m = -INFINITY;
-  for (int s = tid; s < n_split; s += kMergeThreads) m = fmaxf(m, part_m[(size_t)s * rows + row]);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
-  if (tid % 64 == 0) red[tid / 64] = m;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kMergeThreads / 64; ++w) m = fmaxf(m, red[w]);
   f32x4 acc = {};
-  float l = 0.f;
-#pragma unroll 4
-  for (int s = grp; s < n_split; s += G) {
-    const size_t at = (size_t)s * rows + row;
-    const float ls = part_l[at];
-    const float w = ls == 0.f ? 0.f : __builtin_amdgcn_exp2f(part_m[at] - m);
-    acc += w * *reinterpret_cast<const f32x4*>(part_o + at * D + 4 * c);
-    l = fmaf(w, ls, l);
+  float m = -INFINITY, l = 0.f;
+  for (int s0 = grp; s0 < n_split; s0 += U * G) {
+    float ms[U], ls[U];
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + u * G;
+      const size_t at = (size_t)min(s, n_split - 1) * rows + row;
+      ms[u] = part_m[at];
+      ls[u] = s < n_split ? part_l[at] : 0.f;
+      x[u] = *reinterpret_cast<const f32x4*>(part_o + at * D + 4 * c);
+    }
+    float m_new = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, ms[u]);
+    const float alpha = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+    acc *= alpha;
+    l *= alpha;
+    m = m_new;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {  // (l = 0: no key; NaN stays)
+      if (ls[u] == 0.f) continue;
+      const float w = __builtin_amdgcn_exp2f(ms[u] - m);
+      acc += w * x[u];
+      l = fmaf(w, ls[u], l);
+    }
   }
   acc_lds[tid] = acc;
-  if (c == 0) l_lds[grp] = l;
+  if (c == 0) {
+    m_lds[grp] = m;
+    l_lds[grp] = l;
+  }
   __syncthreads();
   if (grp != 0) return;
+  m = m_lds[0];
 #pragma unroll
-  for (int k = 1; k < G; ++k) {
-    acc += acc_lds[k * TPR + tid];
-    l += l_lds[k];
+  for (int k = 1; k < G; ++k) m = fmaxf(m, m_lds[k]);
+  acc = f32x4{};
+  l = 0.f;
+#pragma unroll
+  for (int k = 0; k < G; ++k) {
+    const float lk = l_lds[k];
+    const float w = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(m_lds[k] - m);
+    acc += w * acc_lds[k * TPR + tid];
+    l = fmaf(w, lk, l);
   }
   *reinterpret_cast<f32x4*>(o + (size_t)row * D + 4 * c) = acc * (l == 0.f ? 0.f : 1.f / l);
   if (tid == 0) lse[row] = l == 0.f ? -INFINITY : 0.69314718055994531f * (m + log2f(l));
 }
 
-template <int D, int RB>
-void launch_rows(const Dec4Params& p, unsigned grid, hipStream_t stream) {
-  constexpr int WK = 4;
-  if (p.n_split == 1)
-    hipLaunchKernelGGL((decode4_kernel<D, RB, WK, true>), dim3(grid), dim3(64 * WK), 0, stream, p);
+template <int D, bool WHOLE>
+void launch_splits(const Dec4Params& p, const Decode4Plan& pl, dim3 grid, hipStream_t stream) {
+  if (pl.rows == 16)
+    hipLaunchKernelGGL((decode4_kernel<D, 1, 4, WHOLE>), grid, dim3(256), 0, stream, p);
+  else if (pl.rows == 32)
+    hipLaunchKernelGGL((decode4_kernel<D, 2, 4, WHOLE>), grid, dim3(256), 0, stream, p);
+  else if (pl.rows == 64)
+    hipLaunchKernelGGL((decode4_shared_kernel<D, 2, WHOLE>), grid, dim3(512), 0, stream, p);
   else
-    hipLaunchKernelGGL((decode4_kernel<D, RB, WK, false>), dim3(grid), dim3(64 * WK), 0, stream, p);
+    hipLaunchKernelGGL((decode4_shared_kernel<D, 4, WHOLE>), grid, dim3(512), 0, stream, p);
 }
 
 template <int D>
-hipError_t launch_d(const Dec4Params& p, const Decode4Plan& pl, int n_kv, hipStream_t stream) {
-  const unsigned grid = (unsigned)((int64_t)pl.n_split * pl.row_blocks * n_kv);
-  if (pl.rb == 1) launch_rows<D, 1>(p, grid, stream);
-  else if (pl.rb == 2) launch_rows<D, 2>(p, grid, stream);
-  else launch_rows<D, 4>(p, grid, stream);
+hipError_t launch_d(const Dec4Params& p, const Decode4Plan& pl, hipStream_t stream) {
+  const dim3 grid((unsigned)((int64_t)pl.n_split * pl.row_blocks * p.n_kv));
+  if (pl.n_split == 1) launch_splits<D, true>(p, pl, grid, stream);
+  else launch_splits<D, false>(p, pl, grid, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || pl.n_split == 1) return e;
   hipLaunchKernelGGL((decode4_merge_kernel<D>), dim3((unsigned)p.rows_total), dim3(kMergeThreads), 0,
@@ -488,13 +682,13 @@ hipError_t launch_decode4(const Decode4Args& a, hipStream_t stream) {
   p.part_m = p.part_o + parts * a.head_dim;
   p.part_l = p.part_m + parts;
   p.o = a.o; p.lse = a.lse;
-  p.capacity = a.capacity; p.Lc = a.Lc; p.n_new = a.n_new; p.causal = a.causal;
+  p.capacity = a.capacity; p.Lc = a.Lc; p.n_new = a.n_new; p.causal = a.causal; p.n_kv = a.n_kv;
   p.R = a.n_q / a.n_kv * a.n_new;
   p.rows_total = (int)rows;
   p.n_split = pl.n_split; p.n_rb = pl.row_blocks; p.blocks_per_split = pl.blocks_per_split;
   p.scale_log2 = a.scale_log2;
-  return a.head_dim == 128 ? launch_d<128>(p, pl, a.n_kv, stream)
-                           : launch_d<64>(p, pl, a.n_kv, stream);
+  return a.head_dim == 128 ? launch_d<128>(p, pl, stream)
+                           : launch_d<64>(p, pl, stream);
 }
 
 }  // namespace apb

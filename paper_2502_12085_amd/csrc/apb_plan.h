@@ -151,27 +151,38 @@ inline DecodePlan plan_decode(int64_t n_q, int64_t n_kv, int head_dim, int64_t c
   return pl;
 }
 
-// How a decode call over a 4-bit cache goes about it: 16 * rb rows of a KV head per
-// workgroup, whose four waves take the 32-key blocks of a split in turn.  The workspace
-// holds a partial per split and row: fp32 O, maximum and sum.
+// How a decode call over a 4-bit cache goes about it.  The workspace holds a partial
+// per split and row: fp32 O, maximum and sum.
 struct Decode4Plan {
   int n_split;
-  int blocks_per_split;
-  int rb;          // 16-row blocks of a workgroup (1, 2 or 4)
-  int row_blocks;  // workgroups along the rows of a KV head
+  int blocks_per_split;  // 32-key blocks
+  int rows;              // rows of a KV head per workgroup: 16 or 32 (four waves, each with
+                         // blocks of its own), 64 or 128 (eight that share them)
+  int row_blocks;        // workgroups along the rows of a KV head
   uint64_t workspace_bytes;
 };
 
+#ifndef APB4_T
+#define APB4_T 2
+#endif
+#ifndef APB4_T2
+#define APB4_T2 1
+#endif
+#ifndef APB4_MAXROWS
+#define APB4_MAXROWS 128
+#endif
 inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t cache_len,
                                 int64_t n_new) {
   Decode4Plan pl;
   const int64_t R = n_q / n_kv * n_new, nblk = (cache_len + 31) / 32;
-  pl.rb = R <= 16 ? 1 : R <= 32 ? 2 : 4;
-  pl.row_blocks = (int)((R + 16 * pl.rb - 1) / (16 * pl.rb));
-  // two workgroups per CU, each wave with a block at least
-  int64_t n_split = std::min<int64_t>(2 * kCus / (n_kv * pl.row_blocks), (nblk + 3) / 4);
+  pl.rows = R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128;
+  if (pl.rows > APB4_MAXROWS) pl.rows = APB4_MAXROWS;
+  pl.row_blocks = (int)((R + pl.rows - 1) / pl.rows);
+  // workgroups of one round, each wave (or step) with a block at least
+  const int64_t target = kCus * (pl.rows == 16 ? APB4_T : pl.rows == 32 ? APB4_T2 : 1);
+  int64_t n_split = std::min<int64_t>(target / (n_kv * pl.row_blocks), (nblk + 3) / 4);
   n_split = std::max<int64_t>(n_split, 1);
-  int64_t bps = std::max<int64_t>((nblk + n_split - 1) / n_split, 1);
+  const int64_t bps = std::max<int64_t>((nblk + n_split - 1) / n_split, 1);
   n_split = std::max<int64_t>((nblk + bps - 1) / bps, 1);
   pl.n_split = (int)n_split;
   pl.blocks_per_split = (int)bps;
