@@ -28,6 +28,8 @@
 //    passes 2^13.
 #include <math.h>
 
+#include <type_traits>
+
 #include "apb_internal.h"
 #include "apb_plan.h"
 
@@ -104,9 +106,22 @@ __device__ __forceinline__ uint32_t v_lane(int li, int lg) {
   return (uint32_t)(row * 2 * D + 16 * (((li & 3) >> 1) ^ v_swz<D>(row)) + 8 * (li & 1));
 }
 
-// 32 values of one key into its row's four chunks; a group of NaN as zeros.
-__device__ __forceinline__ void put_values(uint32_t at, u32x4 codes, unsigned b, bool flip) {
-  const bool bad = b == 255;
+// The V operand of dim block db: 32 keys, the lane's eight those of its P operand.
+template <int D>
+__device__ __forceinline__ bf16x8 v_operand(uint32_t v_get, int db) {
+  i16x4 part[2];
+#pragma unroll
+  for (int rd = 0; rd < 2; ++rd)
+    part[rd] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_i16x4*)(uintptr_t)((v_get ^ (32u * db)) + (uint32_t)(16 * rd * 2 * D)));
+  return __builtin_bit_cast(bf16x8,
+                            __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A group's 32 elements into its row's four chunks.  A group of NaN goes there as zeros
+// where it is V's: in a product a zero probability would not keep it out.
+__device__ __forceinline__ void put_group(uint32_t at, u32x4 codes, unsigned b, bool flip, bool v) {
+  const bool bad = v && b == 255;
   const float scale = __uint_as_float(bad ? 0u : b << 23);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -179,30 +194,39 @@ struct Rows4 {
           if (c0 + 16 * i + 4 * lg + r >= vis[rb]) s[i][rb][r] = -INFINITY;
   }
 
-  // Logits (element r of tile i: key 16 i + 4 lg + r) to probabilities, in their three
-  // parts as the P operand, and the running maximum and sum.
-  __device__ __forceinline__ void softmax(const f32x4 (&s)[2][RB], float scale, u32x4 (&pr)[RB][3]) {
+  // Logits of SUB 32-key blocks (element r of tile i: key 16 i + 4 lg + r) to
+  // probabilities, in their three parts as the P operand, and the running maximum and sum.
+  // All of them against one maximum: O is rescaled when that rises, and their values are
+  // not in it yet.
+  template <int SUB>
+  __device__ __forceinline__ void softmax(const f32x4 (&s)[SUB][2][RB], float scale,
+                                          u32x4 (&pr)[SUB][RB][3]) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      float e[8], sum;
+      constexpr int N = 8 * SUB;
+      auto logit = [&](int i) __attribute__((always_inline)) { return s[i >> 3][(i >> 2) & 1][rb][i & 3]; };
+      float e[N], sum;
       auto exps = [&]() __attribute__((always_inline)) {
+        sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          e[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][rb][i & 3], scale, -m_run[rb]));
-        sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        for (int i = 0; i < N; ++i)
+          e[i] = __builtin_amdgcn_exp2f(fmaf(logit(i), scale, -m_run[rb]));
+#pragma unroll
+        for (int i = 0; i < N; i += 8)
+          sum += ((e[i] + e[i + 1]) + (e[i + 2] + e[i + 3])) + ((e[i + 4] + e[i + 5]) + (e[i + 6] + e[i + 7]));
       };
       exps();
       if (__any(!(sum <= kSumLimit))) {
-        float mx = s[0][rb][0];
+        float mx = logit(0);
 #pragma unroll
-        for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i >> 2][rb][i & 3]);
+        for (int i = 1; i < N; ++i) mx = fmaxf(mx, logit(i));
         const float m_new = fmaxf(m_run[rb], across_groups_max(mx) * scale);
         if (m_new == -INFINITY) {
           // nothing but keys that the row does not see, and NaN, which stays
           sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float y = s[i >> 2][rb][i & 3];
+          for (int i = 0; i < N; ++i) {
+            const float y = logit(i);
             e[i] = y == -INFINITY ? 0.f : y;
             sum += e[i];
           }
@@ -217,7 +241,7 @@ struct Rows4 {
       }
       l_run[rb] += sum;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < N / 2; ++i) {
         unsigned hi[2], mid[2], lo[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -226,31 +250,18 @@ struct Rows4 {
           mid[t] = __float_as_uint(r1);
           lo[t] = __float_as_uint(r1 - __uint_as_float(mid[t] & 0xFFFF0000u));
         }
-        pr[rb][0][i] = __builtin_amdgcn_perm(hi[1], hi[0], 0x07060302u);
-        pr[rb][1][i] = __builtin_amdgcn_perm(mid[1], mid[0], 0x07060302u);
-        pr[rb][2][i] = __builtin_amdgcn_perm(lo[1], lo[0], 0x07060302u);
+        u32x4(&out)[3] = pr[i >> 2][rb];
+        out[0][i & 3] = __builtin_amdgcn_perm(hi[1], hi[0], 0x07060302u);
+        out[1][i & 3] = __builtin_amdgcn_perm(mid[1], mid[0], 0x07060302u);
+        out[2][i & 3] = __builtin_amdgcn_perm(lo[1], lo[0], 0x07060302u);
       }
     }
   }
 
-  // O^T += V^T P^T over a tile of 32 rows of V in LDS; v_get: the lane's first address.
-  __device__ __forceinline__ void values(uint32_t v_get, const u32x4 (&pr)[RB][3]) {
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-      i16x4 part[2];
-#pragma unroll
-      for (int rd = 0; rd < 2; ++rd)
-        part[rd] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_i16x4*)(uintptr_t)((v_get ^ (32u * db)) + (uint32_t)(16 * rd * 2 * D)));
-      const bf16x8 v = __builtin_bit_cast(
-          bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-      for (int t = 0; t < 3; ++t)
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-          oacc[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, as_bf16(pr[rb][t]), oacc[rb][db],
-                                                                 0, 0, 0);
-    }
+  // O^T += V^T P^T of one dim block, v its V operand: product t of 3 * RB.
+  __device__ __forceinline__ void value_product(const bf16x8& v, const u32x4 (&pr)[RB][3], int db, int t) {
+    f32x4& o = oacc[t % RB][db];
+    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, as_bf16(pr[t % RB][t / RB]), o, 0, 0, 0);
   }
 
   // Values of group g (dims 32 g ..) of key c are NaN: so is O of the rows that see it.
@@ -262,13 +273,18 @@ struct Rows4 {
         if (db / 2 == g && c < vis[rb]) oacc[rb][db] = f32x4{} + NAN;
   }
 
-  // The parts of WK waves over the same rows (this one the wk-th) meet in LDS at o_lds, 16
-  // bytes a lane for each dim block and wave, and ml_lds; then dim block db goes out from
-  // wave db % WK.
+  // The parts of WK waves over the same rows (this one the wk-th) meet in LDS: at o_lds, 1
+  // KiB for each row block, dim block and wave, and ml_lds.  Then every wave takes 1 / WK of
+  // the rows, whole ones: a store is 1 KiB that lies together.  Chunk 4 db + lg of row li
+  // sits at chunk li ^ (that & 15) of its KiB's quarter lg, on a bank of its own in both
+  // directions.
   template <int WK, bool WHOLE>
   __device__ __forceinline__ void finish(const Dec4Params& p, const Place4& at, int row0, int wk,
                                          uint8_t* o_lds, float (*ml_lds)[WK][RB][16]) {
-    constexpr int OUT = RB * NDB * 4 * 64 * 4;  // bytes of a wave's O
+    constexpr int OUT = RB * NDB * 1024;          // bytes of a wave's O
+    constexpr int CH = D / 4, RPI = 64 / CH;      // chunks of a row, rows of a store
+    constexpr int ROWS = 16 * RB / WK;            // rows of a wave
+    static_assert(ROWS % RPI == 0, "whole stores");
     const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {  // sums over the four lanes of a row
@@ -280,45 +296,42 @@ struct Rows4 {
     for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
-        *reinterpret_cast<f32x4*>(o_lds + wk * OUT + 1024 * (rb * NDB + db) + 16 * lane) = oacc[rb][db];
+        *reinterpret_cast<f32x4*>(o_lds + wk * OUT + 1024 * (rb * NDB + db) + 256 * lg +
+                                  16 * (li ^ ((4 * db + lg) & 15))) = oacc[rb][db];
       if (lg == 0) {
         ml_lds[0][wk][rb][li] = m_run[rb];
         ml_lds[1][wk][rb][li] = l_run[rb];
       }
     }
     __syncthreads();
+    const int c = lane % CH;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int rho = row0 + 16 * rb + li;
-      if (rho >= p.R) continue;
-      float m = -INFINITY, l = 0.f, w[WK];
+    for (int it = 0; it < ROWS / RPI; ++it) {
+      const int r = wk * ROWS + it * RPI + lane / CH, rb = r / 16, ri = r % 16;
+      if (row0 + r >= p.R) continue;
+      float m = -INFINITY, l = 0.f;
 #pragma unroll
-      for (int k = 0; k < WK; ++k) m = fmaxf(m, ml_lds[0][k][rb][li]);
+      for (int k = 0; k < WK; ++k) m = fmaxf(m, ml_lds[0][k][rb][ri]);
+      f32x4 y = {};
 #pragma unroll
       for (int k = 0; k < WK; ++k) {
-        const float lk = ml_lds[1][k][rb][li];  // (0: no key; NaN stays)
-        w[k] = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml_lds[0][k][rb][li] - m);
-        l = fmaf(w[k], lk, l);
+        const float lk = ml_lds[1][k][rb][ri];  // (0: no key; NaN stays)
+        const float w = lk == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml_lds[0][k][rb][ri] - m);
+        l = fmaf(w, lk, l);
+        y += w * *reinterpret_cast<const f32x4*>(o_lds + k * OUT + 1024 * (rb * NDB + c / 4) +
+                                                 256 * (c & 3) + 16 * (ri ^ (c & 15)));
       }
-      const size_t row = (size_t)at.kvh * p.R + rho;
-      const float inv = !WHOLE ? 1.f : l == 0.f ? 0.f : 1.f / l;
-      float* out = (WHOLE ? p.o : p.part_o + (size_t)at.split * p.rows_total * D) + row * D + 4 * lg;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) {
-        if (db % WK != wk) continue;
-        f32x4 y = {};
-#pragma unroll
-        for (int k = 0; k < WK; ++k)
-          y += w[k] *
-               *reinterpret_cast<const f32x4*>(o_lds + k * OUT + 1024 * (rb * NDB + db) + 16 * lane);
-        *reinterpret_cast<f32x4*>(out + 16 * db) = y * inv;
-      }
-      if (wk == 0 && lg == 0) {
-        if constexpr (WHOLE) {
+      const size_t row = (size_t)at.kvh * p.R + row0 + r;
+      if constexpr (WHOLE) {
+        *reinterpret_cast<f32x4*>(p.o + row * D + 4 * c) = y * (l == 0.f ? 0.f : 1.f / l);
+        if (c == 0)
           p.lse[row] = l == 0.f ? -INFINITY : 0.69314718055994531f * (m + log2f(l));
-        } else {
-          p.part_m[(size_t)at.split * p.rows_total + row] = m;
-          p.part_l[(size_t)at.split * p.rows_total + row] = l;
+      } else {
+        const size_t part = (size_t)at.split * p.rows_total + row;
+        *reinterpret_cast<f32x4*>(p.part_o + part * D + 4 * c) = y;
+        if (c == 0) {
+          p.part_m[part] = m;
+          p.part_l[part] = l;
         }
       }
     }
@@ -396,7 +409,7 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
     if (b + WK < b1) next = load(b + WK);
     const int c0 = 32 * b;
 
-    f32x4 s[2][RB];  // S^T: element r of tile i is key c0 + 16 i + 4 lg + r
+    f32x4 s[1][2][RB];  // S^T: element r of tile i is key c0 + 16 i + 4 lg + r
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const float scale = __uint_as_float(x.kb[i] << 23);  // b = 255: NaN elements
@@ -406,25 +419,32 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
           const f32x4 zero = {};
-          s[i][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[rb][j],
-                                                             j == 0 ? zero : s[i][rb], 0, 0, 0);
+          s[0][i][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[rb][j],
+                                                                j == 0 ? zero : s[0][i][rb], 0, 0, 0);
         }
       }
     }
 
-    // V -> LDS.  A group of NaN goes there as zeros, and into O by hand, for the
-    // rows that see it: in a product a zero probability would not keep it out.
+    // V -> LDS; a group of NaN goes into O by hand, for the rows that see it.
     bool bad = false;
 #pragma unroll
     for (int v = 0; v < VL; ++v) bad |= x.vb[v] == 255;
     const bool any_bad = __any(bad);
 #pragma unroll
-    for (int v = 0; v < VL; ++v) put_values(v_put[v], x.vw[v], x.vb[v], flip);
+    for (int v = 0; v < VL; ++v) put_group(v_put[v], x.vw[v], x.vb[v], flip, true);
+    // (a wave's LDS accesses are in order; the reads land during the softmax)
+    bf16x8 v[Rows::NDB];
+#pragma unroll
+    for (int db = 0; db < Rows::NDB; ++db) v[db] = v_operand<D>(v_get, db);
+    __builtin_amdgcn_sched_barrier(0);
 
-    if (c0 + 32 > vis_all) rows.mask(s, c0, lg);
-    u32x4 pr[RB][3];
+    if (c0 + 32 > vis_all) rows.mask(s[0], c0, lg);
+    u32x4 pr[1][RB][3];
     rows.softmax(s, p.scale_log2, pr);
-    rows.values(v_get, pr);
+#pragma unroll
+    for (int db = 0; db < Rows::NDB; ++db)
+#pragma unroll
+      for (int t = 0; t < 3 * RB; ++t) rows.value_product(v[db], pr[0], db, t);
 
     if (any_bad) {  // the first key of each group's NaN
 #pragma unroll
@@ -443,131 +463,195 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
 }
 
 // More rows: eight waves, WR of them with 32 rows each and WK = 8 / WR such sets, which
-// take a split's keys in turn.  A step is 128 keys: all threads make its codes bf16
-// and put K and V into LDS, where each set reads 128 / WK of them, so that the work of a
-// conversion is shared by 32 * WR rows.  The next step's codes are in flight and its
-// conversion is among this one's products; two buffers, one barrier a step.
+// share a split's keys.  A step is 128 keys: all threads make its codes bf16 and put K
+// and V into LDS, where each set reads 128 / WK of them, so that the work of a conversion
+// is shared by 32 * WR rows.
+// Products and vector work are about even here (a 32-key block of 32 rows: 64 products of
+// 16 cycles; 200 vector instructions of 4 and 16 exponentials of 16), and eight waves in
+// step would wait for each other's turns at both.  So the waves form two groups, one wave
+// of each on every SIMD, and a barrier ends every phase:
+//   phase    group A                       group B
+//   2 t      S(t) = Q K(t), O += P V(t-1)  softmax(t-1); K(t+1), V(t) -> LDS
+//   2 t + 1  softmax(t); K(t+1), V(t)      S(t), O += P V(t-1)
+//            -> LDS
+// K(t) and V(t-1) are read in both phases while K(t+1) and V(t) are written: two buffers
+// of each.  The codes of the writes after those are in flight meanwhile.
 template <int D, int WR, bool WHOLE>
 __global__ void __launch_bounds__(512, 2) decode4_shared_kernel(Dec4Params p) {
   constexpr int RB = 2, WK = 8 / WR, SUB = 4 / WK;  // 32-key blocks of a step and set
   using Rows = Rows4<D, RB>;
   constexpr int KW = D / 32, G = D / 32, TILE = 32 * D * 2;
-  constexpr int UNITS = 128 * G / 512 > 0 ? 1 : 0;  // of K and of V in each thread, or K or V
-  static_assert(UNITS == (D == 128), "a thread's share of a step");
-  __shared__ __attribute__((aligned(256))) uint8_t lds[2][2][4][TILE];  // buffer, K or V, block
+  __shared__ __attribute__((aligned(256))) uint8_t lds[2][2][4][TILE];  // K or V, buffer, block
   __shared__ float ml_lds[WR][2][WK][RB][16];
   // First key (of 32) whose values of a group are NaN, and whether there is one, by step % 3:
-  // cleared in the step before it is set.
+  // cleared in the step before it is set, read in the one after.
   __shared__ int nan_lds[3][4][4], any_lds[3];
 
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
+  const bool group_b = wave >= 4;
   const Place4 at = place4(p.n_split, p.n_rb, p.n_kv);
   const int nblk = (p.Lc + 31) / 32;
   const int b0 = at.split * p.blocks_per_split, b1 = min(b0 + p.blocks_per_split, nblk);
   const int steps = (b1 - b0 + 3) / 4;
-  const int vis_all = p.causal ? p.Lc - p.n_new + 1 : p.Lc;
+  const int vis_all = min(p.causal ? p.Lc - p.n_new + 1 : p.Lc, 32 * b1);
 
-  // This thread's groups of a step: (key, g) of K and of V (d = 128), or of one of them.
-  const int unit = D == 128 ? tid : tid & 255, key = unit / G, g = unit % G;
-  const bool has_k = D == 128 || tid < 256, has_v = D == 128 || tid >= 256;
+  // This thread's groups of a step: (key, g) of K and of V (d = 128), or of one of them by
+  // wave (d = 64).  Every load and write is made, whatever the step: past the split's end
+  // they repeat its last key and go where nothing is read any more.  (Where some are
+  // left out, the compiler waits for all that are in flight before the first is used.)
+  constexpr int NU = D / 64;
+  const int unit = D == 128 ? tid : (tid & 63) + (tid >> 7) * 64, key = unit / G, g = unit % G;
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-  const uint32_t row = (uint32_t)(key * 2 * D);  // (blocks follow one another)
-  const uint32_t k_put = base + row + 16u * ((4 * g) ^ k_swz<D>(key));
-  const uint32_t v_put = base + 4 * TILE + row + 16u * ((4 * g) ^ v_swz<D>(key) ^ v_flip<D>(key));
-  const bool flip = v_flip<D>(key) != 0;
-  constexpr uint32_t BUF = 8 * TILE;
+  constexpr uint32_t BUF = 4 * TILE, V = 2 * BUF;
+  bool is_v[NU], flip[NU];
+  uint32_t put_at[NU];
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    is_v[u] = D == 128 ? u == 1 : (wave & 1) != 0;
+    flip[u] = is_v[u] && v_flip<D>(key) != 0;
+    const int swz = is_v[u] ? v_swz<D>(key) ^ v_flip<D>(key) : k_swz<D>(key);
+    put_at[u] = base + (is_v[u] ? V : 0) + (uint32_t)(key * 2 * D) + 16u * ((4 * g) ^ swz);
+  }
 
-  u32x4 kw = {}, vw = {};
-  unsigned kb = 0, vb = 0;
-  auto load = [&](int step) __attribute__((always_inline)) {
-    const int c0 = 32 * (b0 + 4 * step);
-    const uint32_t k = (uint32_t)min(key, p.Lc - 1 - c0);  // rows past the last key repeat it
-    const size_t r0 = (size_t)at.kvh * p.capacity + c0;
-    if (has_k) {
-      kw = *reinterpret_cast<const u32x4*>(p.k_codes + r0 * (D / 2) + (k * (D / 2) + 16u * g));
-      kb = (p.k_scales + r0 * G)[k * G + g];
-    }
-    if (has_v) {
-      vw = *reinterpret_cast<const u32x4*>(p.v_codes + r0 * (D / 2) + (k * (D / 2) + 16u * g));
-      vb = (p.v_scales + r0 * G)[k * G + g];
+  struct Unit {
+    u32x4 w;
+    unsigned b;
+  };
+  // The codes of K(step) and V(step - 1), and their way into LDS.
+  auto load = [&](int step, Unit (&x)[NU]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const int c0 = min(32 * (b0 + 4 * max(step - (is_v[u] ? 1 : 0), 0)), p.Lc - 1);
+      const uint32_t k = (uint32_t)min(key, p.Lc - 1 - c0);
+      const size_t r0 = (size_t)at.kvh * p.capacity + c0;
+      const uint8_t* codes = (is_v[u] ? p.v_codes : p.k_codes) + r0 * (D / 2);
+      const uint8_t* scales = (is_v[u] ? p.v_scales : p.k_scales) + r0 * G;
+      x[u].w = *reinterpret_cast<const u32x4*>(codes + (k * (D / 2) + 16u * g));
+      x[u].b = scales[k * G + g];
     }
   };
-  auto put = [&](int step) __attribute__((always_inline)) {
-    const uint32_t buf = step & 1 ? BUF : 0;
-    if (has_k) {
-      const float scale = __uint_as_float(kb << 23);
+  auto put = [&](int step, const Unit (&x)[NU]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *(lds_u32x4*)(uintptr_t)((k_put + buf) ^ (16u * j)) = elements(kw[j], scale);
-    }
-    if (has_v) {
-      put_values(v_put + buf, vw, vb, flip);
-      if (vb == 255) {
-        atomicMin(&nan_lds[step % 3][key / 32][g], key % 32);
-        any_lds[step % 3] = 1;
+    for (int u = 0; u < NU; ++u) {
+      const int of = step - (is_v[u] ? 1 : 0);
+      put_group(put_at[u] + (of & 1 ? BUF : 0), x[u].w, x[u].b, flip[u], is_v[u]);
+      if (is_v[u] && x[u].b == 255 && of < steps) {
+        atomicMin(&nan_lds[of % 3][key / 32][g], key % 32);
+        any_lds[of % 3] = 1;
       }
     }
   };
-  auto clear = [&](int step) __attribute__((always_inline)) {
-    if (tid < 16) nan_lds[step % 3][tid / 4][tid % 4] = 32;
-    if (tid == 16) any_lds[step % 3] = 0;
+  auto put_keys = [&](const Unit (&x)[NU]) __attribute__((always_inline)) {  // K(0)
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+      if (!is_v[u]) put_group(put_at[u], x[u].w, x[u].b, false, false);
+  };
+  auto clear = [&](int step) __attribute__((always_inline)) {  // by group B
+    if (tid >= 256 && tid < 272) nan_lds[step % 3][(tid & 15) / 4][tid & 3] = 32;
+    if (tid == 272) any_lds[step % 3] = 0;
   };
 
   Rows rows;
   const int row0 = 32 * (WR * at.row_block + wr);
-  const bool has_rows = row0 < p.R;
-  rows.start(p, at.kvh, row0, [&](int j) { return 32 * j + 8 * lg; });
-  const uint32_t v_get = base + 4 * TILE + v_lane<D>(li, lg);
-  const uint32_t k_get = base + (uint32_t)(li * 2 * D) + 16u * (lg ^ k_swz<D>(li));
-
+  Unit codes[NU], first[NU];
   if (steps > 0) {
-    load(0);
-    clear(0);
-    clear(1);
-    __syncthreads();
-    put(0);
-    if (steps > 1) load(1);
+    load(0, first);
+    load(1, codes);
   }
+  rows.start(p, at.kvh, row0, [&](int j) { return 32 * j + 8 * lg; });
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) rows.vis[rb] = min(rows.vis[rb], 32 * b1);
+  const uint32_t k_get = base + (uint32_t)(li * 2 * D) + 16u * (lg ^ k_swz<D>(li)) + wk * SUB * TILE;
+  const uint32_t v_get = base + V + v_lane<D>(li, lg) + wk * SUB * TILE;
+
+  clear(0);
+  if (steps > 0) put_keys(first);
   __syncthreads();
-  for (int step = 0; step < steps; ++step) {
-    if (step + 1 < steps) {
-      put(step + 1);
-      if (step + 2 < steps) load(step + 2);
-    }
-    clear(step + 2);
-    const bool any_bad = any_lds[step % 3] != 0;
-    const uint32_t buf = step & 1 ? BUF : 0;
+  if (group_b && steps > 0) {
+    put(1, codes);
+    load(2, codes);
+    clear(1);
+  }
+  f32x4 s[SUB][2][RB];
+  u32x4 pr[SUB][RB][3];
+  // A phase of products, in turns of two dim blocks of O (twelve, on four accumulators) and
+  // two operands of S (four): a turn's operands are read while the one before it goes on.
+  auto products = [&](int step, auto with_s, auto with_o) __attribute__((always_inline)) {
+    constexpr bool S = decltype(with_s)::value, O = decltype(with_o)::value;
+    constexpr int N = Rows::NDB * SUB / 2;
+    static_assert(Rows::NDB == 2 * KW, "as many dim blocks as operands of K");
+    const uint32_t kt = k_get + (step & 1 ? BUF : 0), vt = v_get + (step & 1 ? 0 : BUF);
+    bf16x8 k[2][2], v[2][2];
+    auto read = [&](int n) __attribute__((always_inline)) {
+      const int t = 2 * n / Rows::NDB, m = 2 * n % Rows::NDB;
 #pragma unroll
-    for (int t = 0; t < SUB; ++t) {
-      const int blk = wk * SUB + t, b = b0 + 4 * step + blk, c0 = 32 * b;
-      if (b >= b1 || !has_rows) continue;
-      const uint32_t kt = k_get + buf + blk * TILE;
-      f32x4 s[2][RB];
+      for (int i = 0; i < 2; ++i) {
+        if constexpr (O) v[n & 1][i] = v_operand<D>(vt + t * TILE, m + i);
+        if constexpr (S)
+          k[n & 1][i] = as_bf16(*(lds_u32x4*)(uintptr_t)((kt ^ (64u * (m / 2))) +
+                                                        (uint32_t)(t * TILE + 16 * i * 2 * D)));
+      }
+    };
+    read(0);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+    for (int n = 0; n < N; ++n) {
+      const int t = 2 * n / Rows::NDB, m = 2 * n % Rows::NDB, j = m / 2;
+      if (n + 1 < N) read(n + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < KW; ++j) {
-          const bf16x8 k = as_bf16(*(lds_u32x4*)(uintptr_t)((kt ^ (64u * j)) + (uint32_t)(16 * i * 2 * D)));
+      for (int u = 0; u < 3; ++u) {
+        if constexpr (O) {
 #pragma unroll
-          for (int rb = 0; rb < RB; ++rb) {
-            const f32x4 zero = {};
-            s[i][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, rows.q[rb][j],
-                                                               j == 0 ? zero : s[i][rb], 0, 0, 0);
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) rows.value_product(v[n & 1][i], pr[t], m + i, RB * u + rb);
+        }
+        if constexpr (S) {
+          if (u < 2) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+              const f32x4 zero = {};
+              s[t][u][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  k[n & 1][u], rows.q[rb][j], j == 0 ? zero : s[t][u][rb], 0, 0, 0);
+            }
           }
         }
-      if (c0 + 32 > vis_all) rows.mask(s, c0, lg);
-      u32x4 pr[RB][3];
-      rows.softmax(s, p.scale_log2, pr);
-      rows.values(v_get + buf + blk * TILE, pr);
-      if (any_bad) {
-        for (int n = 0; n < G; ++n) {
-          const int first = nan_lds[step % 3][blk][n];
-          if (first < 32) rows.not_a_number(n, c0 + first);
-        }
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __syncthreads();
+  };
+  auto not_numbers = [&](int step, int any) __attribute__((always_inline)) {
+    if (any == 0) return;
+    for (int t = 0; t < SUB; ++t)
+      for (int n = 0; n < G; ++n) {
+        const int blk = wk * SUB + t, first = nan_lds[step % 3][blk][n];
+        if (first < 32) rows.not_a_number(n, 32 * (b0 + 4 * step + blk) + first);
+      }
+  };
+  auto turn = [&](int step, auto more) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < SUB; ++t) {
+      const int c0 = 32 * (b0 + 4 * step + wk * SUB + t);
+      if (c0 + 32 > vis_all) rows.mask(s[t], c0, lg);
+    }
+    rows.softmax(s, p.scale_log2, pr);
+    put(step + (group_b ? 2 : 1), codes);
+    load(step + (group_b ? 3 : 2), codes);
+    if (group_b) clear(step + 2);
+    if (!group_b) __syncthreads();
+    const int any = any_lds[step % 3];
+    __builtin_amdgcn_s_setprio(1);
+    products(step + 1, more, std::true_type{});
+    __builtin_amdgcn_s_setprio(0);
+    not_numbers(step, any);
+    if (decltype(more)::value && group_b) __syncthreads();
+  };
+  if (steps > 0) {
+    products(0, std::true_type{}, std::false_type{});
+    if (group_b) __syncthreads();
+    for (int step = 0; step + 1 < steps; ++step) turn(step, std::true_type{});
+    turn(steps - 1, std::false_type{});
   }
   rows.template finish<WK, WHOLE>(p, at, row0, wk, &lds[0][0][0][0] + wr * WK * RB * D * 64, ml_lds[wr]);
 }
