@@ -274,8 +274,8 @@ struct Rows4 {
   }
 
   // The parts of WK waves over the same rows (this one the wk-th) meet in LDS: at o_lds, 1
-  // KiB for each row block, dim block and wave, and ml_lds.  Then every wave takes 1 / WK of
-  // the rows, whole ones: a store is 1 KiB that lies together.  Chunk 4 db + lg of row li
+  // KiB for each row block, dim block and wave, and ml_lds.  Then the waves take the
+  // rows in turn, whole ones: a store is 1 KiB that lies together.  Chunk 4 db + lg of row li
   // sits at chunk li ^ (that & 15) of its KiB's quarter lg, on a bank of its own in both
   // directions.
   template <int WK, bool WHOLE>
@@ -283,8 +283,7 @@ struct Rows4 {
                                          uint8_t* o_lds, float (*ml_lds)[WK][RB][16]) {
     constexpr int OUT = RB * NDB * 1024;          // bytes of a wave's O
     constexpr int CH = D / 4, RPI = 64 / CH;      // chunks of a row, rows of a store
-    constexpr int ROWS = 16 * RB / WK;            // rows of a wave
-    static_assert(ROWS % RPI == 0, "whole stores");
+    constexpr int ROWS = 16 * RB, TURNS = (ROWS + RPI * WK - 1) / (RPI * WK);
     const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {  // sums over the four lanes of a row
@@ -306,9 +305,9 @@ struct Rows4 {
     __syncthreads();
     const int c = lane % CH;
 #pragma unroll
-    for (int it = 0; it < ROWS / RPI; ++it) {
-      const int r = wk * ROWS + it * RPI + lane / CH, rb = r / 16, ri = r % 16;
-      if (row0 + r >= p.R) continue;
+    for (int it = 0; it < TURNS; ++it) {
+      const int r = (it * WK + wk) * RPI + lane / CH, rb = r / 16, ri = r % 16;
+      if (r >= ROWS || row0 + r >= p.R) continue;
       float m = -INFINITY, l = 0.f;
 #pragma unroll
       for (int k = 0; k < WK; ++k) m = fmaxf(m, ml_lds[0][k][rb][ri]);
@@ -369,7 +368,7 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
 
   auto load = [&](int b) __attribute__((always_inline)) {
     Block4<D> x;
-    const int c0 = 32 * b, last = p.Lc - 1 - c0;  // rows past the last key repeat it
+    const int c0 = min(32 * b, p.Lc - 1), last = p.Lc - 1 - c0;  // rows past the last key repeat it
     const size_t r0 = (size_t)at.kvh * p.capacity + c0;
     const uint8_t* kc = p.k_codes + r0 * (D / 2);
     const uint8_t* ks = p.k_scales + r0 * G;
@@ -402,13 +401,12 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
   // (a lane's d / 4 elements of its key lie together)
   rows.start(p, at.kvh, row0, [&](int j) { return lg * (D / 4) + 8 * j; });
 
-  Block4<D> next;
-  if (b0 + wave < b1) next = load(b0 + wave);
-  for (int b = b0 + wave; b < b1; b += WK) {
-    const Block4<D> x = next;
-    if (b + WK < b1) next = load(b + WK);
+  // Block b from x, which takes the wave's next block as soon as it is done with, whatever
+  // b1 (past the last key the loads repeat it).  A second block in flight per wave gained
+  // nothing (16385 keys of 8 heads 11.4 against 12.3 us, 524289 110.8 against 112.2): eight
+  // waves of a CU have 35 KiB under way.
+  auto block = [&](Block4<D>& x, int b) __attribute__((always_inline)) {
     const int c0 = 32 * b;
-
     f32x4 s[1][2][RB];  // S^T: element r of tile i is key c0 + 16 i + 4 lg + r
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -425,13 +423,28 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
       }
     }
 
-    // V -> LDS; a group of NaN goes into O by hand, for the rows that see it.
+    // V -> LDS; a group of NaN goes into O by hand, for the rows that see it: the first
+    // key of each.
+    int first[G];
     bool bad = false;
 #pragma unroll
-    for (int v = 0; v < VL; ++v) bad |= x.vb[v] == 255;
+    for (int v = 0; v < VL; ++v) {
+      put_group(v_put[v], x.vw[v], x.vb[v], flip, true);
+      bad |= x.vb[v] == 255;
+    }
     const bool any_bad = __any(bad);
+    if (any_bad) {
 #pragma unroll
-    for (int v = 0; v < VL; ++v) put_group(v_put[v], x.vw[v], x.vb[v], flip, true);
+      for (int g = 0; g < G; ++g) {
+        first[g] = 32;
+#pragma unroll
+        for (int v = 0; v < VL; ++v) {
+          const unsigned long long hit = __ballot(x.vb[v] == 255 && (int)(lane % G) == g);
+          if (hit) first[g] = min(first[g], (64 * v + (int)__builtin_ctzll(hit)) / G);
+        }
+      }
+    }
+    x = load(b + WK);
     // (a wave's LDS accesses are in order; the reads land during the softmax)
     bf16x8 v[Rows::NDB];
 #pragma unroll
@@ -445,19 +458,15 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
     for (int db = 0; db < Rows::NDB; ++db)
 #pragma unroll
       for (int t = 0; t < 3 * RB; ++t) rows.value_product(v[db], pr[0], db, t);
-
-    if (any_bad) {  // the first key of each group's NaN
+    if (any_bad) {
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        int first = 32;
-#pragma unroll
-        for (int v = 0; v < VL; ++v) {
-          const unsigned long long hit = __ballot(x.vb[v] == 255 && (int)(lane % G) == g);
-          if (hit) first = min(first, (64 * v + (int)__builtin_ctzll(hit)) / G);
-        }
-        if (first < 32) rows.not_a_number(g, c0 + first);
-      }
+      for (int g = 0; g < G; ++g)
+        if (first[g] < 32) rows.not_a_number(g, c0 + first[g]);
     }
+  };
+  if (b0 + wave < b1) {
+    Block4<D> x = load(b0 + wave);
+    for (int b = b0 + wave; b < b1; b += WK) block(x, b);
   }
   rows.template finish<WK, WHOLE>(p, at, row0, wave, lds, ml_lds);
 }
@@ -658,10 +667,10 @@ __global__ void __launch_bounds__(512, 2) decode4_shared_kernel(Dec4Params p) {
 
 // The splits of a row: O = sum_s 2^(m_s - m) O_s / l, l = sum_s 2^(m_s - m) l_s, with m
 // the largest m_s; lse = ln 2 (m + log2 l).  Parts keep O undivided, and m apart from
-// log l: a sum of the two would lose l's digits beside a large m.  A workgroup per row,
-// 16 bytes of O a thread; a thread takes every G-th split, eight at a time against its
-// own maximum, so that all it reads is one trip to memory, and the thread groups meet in
-// LDS.
+// log l: a sum of the two would lose l's digits beside a large m.  16 bytes of O a
+// thread; its G thread groups take every G-th split, eight at a time against their own
+// maximum, so that all a thread reads is one trip to memory, and meet in LDS.  (Two
+// groups and four rows a workgroup: no faster at 2048 rows and 16 splits.)
 constexpr int kMergeThreads = 256;
 
 template <int D>
@@ -725,8 +734,12 @@ __global__ void __launch_bounds__(kMergeThreads) decode4_merge_kernel(
 
 template <int D, bool WHOLE>
 void launch_splits(const Dec4Params& p, const Decode4Plan& pl, dim3 grid, hipStream_t stream) {
-  if (pl.rows == 16)
+  if (pl.rows == 16 && pl.waves == 8)
+    hipLaunchKernelGGL((decode4_kernel<D, 1, 8, WHOLE>), grid, dim3(512), 0, stream, p);
+  else if (pl.rows == 16)
     hipLaunchKernelGGL((decode4_kernel<D, 1, 4, WHOLE>), grid, dim3(256), 0, stream, p);
+  else if (pl.rows == 32 && WHOLE && pl.waves == 8)  // (splits of 32 rows have four)
+    hipLaunchKernelGGL((decode4_kernel<D, 2, 8, true>), grid, dim3(512), 0, stream, p);
   else if (pl.rows == 32)
     hipLaunchKernelGGL((decode4_kernel<D, 2, 4, WHOLE>), grid, dim3(256), 0, stream, p);
   else if (pl.rows == 64)
@@ -743,7 +756,7 @@ hipError_t launch_d(const Dec4Params& p, const Decode4Plan& pl, hipStream_t stre
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || pl.n_split == 1) return e;
   hipLaunchKernelGGL((decode4_merge_kernel<D>), dim3((unsigned)p.rows_total), dim3(kMergeThreads), 0,
-                     stream, pl.n_split, p.rows_total, p.part_o, p.part_m, p.part_l, p.o, p.lse);
+                     stream, p.n_split, p.rows_total, p.part_o, p.part_m, p.part_l, p.o, p.lse);
   return hipGetLastError();
 }
 

@@ -156,36 +156,50 @@ inline DecodePlan plan_decode(int64_t n_q, int64_t n_kv, int head_dim, int64_t c
 struct Decode4Plan {
   int n_split;
   int blocks_per_split;  // 32-key blocks
-  int rows;              // rows of a KV head per workgroup: 16 or 32 (four waves, each with
-                         // blocks of its own), 64 or 128 (eight that share them)
+  int rows;              // rows of a KV head per workgroup: 16 or 32 (its waves have
+                         // blocks of their own), 64 or 128 (they share steps of four)
+  int waves;             // of a workgroup
   int row_blocks;        // workgroups along the rows of a KV head
   uint64_t workspace_bytes;
 };
 
-#ifndef APB4_T
-#define APB4_T 2
-#endif
-#ifndef APB4_T2
-#define APB4_T2 1
-#endif
-#ifndef APB4_MAXROWS
-#define APB4_MAXROWS 128
-#endif
+// Most key blocks of a call that is one launch, the waves of one workgroup per KV head
+// and row block sharing them: up to there it takes as long as two launches on the GPU, and
+// the host is 2 us quicker.  16 rows of d = 128: 10 blocks 6.5 -> 5.3 us, 19 6.7 against
+// 6.8; d = 64: 10 5.8 -> 3.9, 17 6.1 -> 4.9, 32 5.9 against 6.2; 32 rows: 10 9.0 -> 9.0,
+// 19 9.2 against 10.8.
+constexpr int decode4_one_launch_blocks(int rows) { return rows == 16 ? 24 : 12; }
+
 inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t cache_len,
                                 int64_t n_new) {
   Decode4Plan pl;
   const int64_t R = n_q / n_kv * n_new, nblk = (cache_len + 31) / 32;
   pl.rows = R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128;
-  if (pl.rows > APB4_MAXROWS) pl.rows = APB4_MAXROWS;
-  pl.row_blocks = (int)((R + pl.rows - 1) / pl.rows);
-  // workgroups of one round, each wave (or step) with a block at least
-  const int64_t target = kCus * (pl.rows == 16 ? APB4_T : pl.rows == 32 ? APB4_T2 : 1);
-  int64_t n_split = std::min<int64_t>(target / (n_kv * pl.row_blocks), (nblk + 3) / 4);
+  const int64_t row_blocks = (R + pl.rows - 1) / pl.rows;
+  const int64_t per_cu = kCus / (n_kv * row_blocks);  // splits that give every CU a workgroup
+  int64_t n_split;
+  pl.waves = pl.rows > 32 ? 8 : 4;
+  if (pl.rows <= 32 && nblk <= decode4_one_launch_blocks(pl.rows)) {
+    n_split = 1;
+    if (nblk > 4) pl.waves = 8;
+  } else if (pl.rows == 16 && nblk >= 4 * per_cu && per_cu > 0) {
+    // eight waves with a block each in half a round at least: as many waves on a CU as
+    // two workgroups of four, and half the partials (8 heads: 16385 keys 12.3 -> 11.6
+    // us, 4097 8.7 -> 8.5; 2048 7.4 against 8.3)
+    pl.waves = 8;
+    n_split = per_cu;
+  } else {
+    n_split = std::min<int64_t>(pl.rows == 16 ? 2 * per_cu : per_cu, (nblk + 3) / 4);
+  }
   n_split = std::max<int64_t>(n_split, 1);
-  const int64_t bps = std::max<int64_t>((nblk + n_split - 1) / n_split, 1);
+  int64_t bps = std::max<int64_t>((nblk + n_split - 1) / n_split, 1);
+  // whole steps: a part of one takes as long (256 rows: 16448 keys 50.4 -> 47.7 us, 2049
+  // 25.6 -> 22.7)
+  if (pl.rows > 32) bps = (bps + 3) / 4 * 4;
   n_split = std::max<int64_t>((nblk + bps - 1) / bps, 1);
   pl.n_split = (int)n_split;
   pl.blocks_per_split = (int)bps;
+  pl.row_blocks = (int)row_blocks;
   pl.workspace_bytes = (uint64_t)n_split * (uint64_t)(n_q * n_new) * (uint64_t)(head_dim + 2) * 4;
   return pl;
 }
