@@ -413,73 +413,76 @@ def layer_fwd(problem, weights: dict, hidden_in, positions, k_cache, v_cache, pa
 # The elements that a call's sizes ask of each tensor are counted here: a cache
 # is sized by its capacity, not by the rows in use, so a tensor of another size
 # is an easy mistake, and one that the C call cannot see.  Nor can it see a tensor
-# of another device than the current one, whose stream the call would use.  A tensor
-# that is as it should be costs one expression (a call on a few rows takes 2 us of
-# the GPU, so what the host does is what it costs); what is wrong is found after.
-class _Call:
-    """The current device, the types and the stream of one call."""
+# of another device than the current one, whose stream the call would use.  A call
+# on a few rows takes 2 us of the GPU, so what the host does is what it costs: a
+# tensor that is as it should be is one expression, and what is wrong is found after.
+class _Cuda:
+    """Types and lookups, filled in by ``_device``."""
 
-    __slots__ = ("where", "check", "problem", "dev")
-
-    def __init__(self, where, check, problem):
-        self.where, self.check, self.problem = where, check, problem
-        self.dev = _device()
-
-    def ptr(self, t, name, types, n):
-        if t is None:
-            return None
-        if (t.dtype in types and t.numel() == n and t.get_device() == self.dev
-                and t.is_contiguous()):
-            return t.data_ptr()
-        _check(self.check(self.problem), self.where)  # sizes that are wrong in themselves
-        _ptr(t, name, types)
-        if t.get_device() != self.dev:
-            raise ValueError(f"{name} is on {t.device}, not on the current device")
-        raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
-
-    def cache(self, c, n_kv, capacity, d):
-        codes, scales, u = n_kv * capacity * (d // 2), n_kv * capacity * (d // 32), _types().u8
-        return Cache4(self.ptr(c["k_codes"], "k_codes", u, codes),
-                      self.ptr(c["k_scales"], "k_scales", u, scales),
-                      self.ptr(c["v_codes"], "v_codes", u, codes),
-                      self.ptr(c["v_scales"], "v_scales", u, scales))
-
-    def stream(self, stream):
-        if stream is None and _types().raw_stream is not None:
-            return _types().raw_stream(self.dev)
-        return _stream(stream)
-
-
-class _Types:
-    def __init__(self):
-        import torch
-        self.bf16, self.f32, self.u8 = _bf16_types(), (torch.float32,), (torch.uint8,)
-        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        self.raw_device = getattr(torch._C, "_cuda_getDevice", None)
-        self.ready = False
-
-
-_known_types = None
-
-
-def _types():
-    global _known_types
-    if _known_types is None:
-        _known_types = _Types()
-    return _known_types
+    bf16 = f32 = raw_stream = raw_device = u8 = None
 
 
 def _device():
     """The current device's index; -2 where there is none (no tensor's device)."""
-    t = _types()
-    if t.ready:
-        return t.raw_device()
+    if _Cuda.raw_device is not None:
+        return _Cuda.raw_device()
     import torch
+    _Cuda.bf16, _Cuda.f32, _Cuda.u8 = _bf16_types(), torch.float32, torch.uint8
     if not torch.cuda.is_available():
         return -2
     dev = torch.cuda.current_device()  # initialises the runtime
-    t.ready = t.raw_device is not None
+    _Cuda.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _Cuda.raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     return dev
+
+
+def _wrong(t, name, types, n, dev, status, where):
+    """Raises what is wrong with a tensor of a call, whose sizes have `status`."""
+    _check(status, where)  # sizes that are wrong in themselves
+    _ptr(t, name, types)
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
+
+
+def _rows4(t, name, n, dev, validate, problem, where):
+    """Device pointer of a bf16 tensor of n elements, or None."""
+    if t is None:
+        return None
+    if (t.dtype in _Cuda.bf16 and t.numel() == n and t.get_device() == dev
+            and t.is_contiguous()):
+        return t.data_ptr()
+    return _wrong(t, name, _Cuda.bf16, n, dev, validate(problem), where)
+
+
+def _cache4(cache, dev, validate, problem, where):
+    """``apb_cache4_t`` of a mapping of the four tensors (uint8)."""
+    rows, d, u8 = problem.n_kv_heads * problem.capacity, problem.head_dim, _Cuda.u8
+    codes, scales = rows * (d // 2), rows * (d // 32)
+    kc, ks, vc, vs = (cache["k_codes"], cache["k_scales"], cache["v_codes"], cache["v_scales"])
+    if (kc is not None and ks is not None and vc is not None and vs is not None
+            and kc.dtype is u8 and ks.dtype is u8 and vc.dtype is u8 and vs.dtype is u8
+            and kc.numel() == codes and vc.numel() == codes
+            and ks.numel() == scales and vs.numel() == scales
+            and kc.get_device() == dev and vc.get_device() == dev
+            and ks.get_device() == dev and vs.get_device() == dev
+            and kc.is_contiguous() and vc.is_contiguous()
+            and ks.is_contiguous() and vs.is_contiguous()):
+        return Cache4(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr())
+    for name, n in (("k_codes", codes), ("k_scales", scales), ("v_codes", codes),
+                    ("v_scales", scales)):
+        t = cache[name]
+        if t is None:
+            _check(validate(problem) or 1, where)
+        if not (t.dtype is u8 and t.numel() == n and t.get_device() == dev
+                and t.is_contiguous()):
+            _wrong(t, name, (u8,), n, dev, validate(problem), where)
+
+
+def _stream4(stream, dev):
+    if stream is None and _Cuda.raw_stream is not None:
+        return _Cuda.raw_stream(dev)
+    return _stream(stream)
 
 
 def validate_cache4(problem) -> int:
@@ -490,25 +493,27 @@ def cache4_write(problem, k, v, cache: dict, stream=None):
     """``apb_cache4_write``: quantise rows of ``k``/``v`` [n_kv, bf16_rows, d]
     (bf16) into ``cache``, a mapping of ``k_codes``/``v_codes`` [n_kv, capacity,
     d / 2] and ``k_scales``/``v_scales`` [n_kv, capacity, d / 32] (uint8)."""
-    c, b = _Call("apb_cache4_write", validate_cache4, problem), _types().bf16
-    n_kv, d = problem.n_kv_heads, problem.head_dim
-    n = n_kv * problem.bf16_rows * d
-    st = lib().apb_cache4_write(problem, c.ptr(k, "k", b, n), c.ptr(v, "v", b, n),
-                                c.cache(cache, n_kv, problem.capacity, d), c.stream(stream))
+    dev, where = _device(), "apb_cache4_write"
+    n = problem.n_kv_heads * problem.bf16_rows * problem.head_dim
+    st = lib().apb_cache4_write(problem, _rows4(k, "k", n, dev, validate_cache4, problem, where),
+                                _rows4(v, "v", n, dev, validate_cache4, problem, where),
+                                _cache4(cache, dev, validate_cache4, problem, where),
+                                _stream4(stream, dev))
     if st:
-        _check(st, "apb_cache4_write")
+        _check(st, where)
 
 
 def cache4_read(problem, cache: dict, k, v, stream=None):
     """``apb_cache4_read``: the values of cache rows into ``k``/``v`` [n_kv,
     bf16_rows, d] (bf16); ``cache`` as in ``cache4_write``."""
-    c, b = _Call("apb_cache4_read", validate_cache4, problem), _types().bf16
-    n_kv, d = problem.n_kv_heads, problem.head_dim
-    n = n_kv * problem.bf16_rows * d
-    st = lib().apb_cache4_read(problem, c.cache(cache, n_kv, problem.capacity, d),
-                               c.ptr(k, "k", b, n), c.ptr(v, "v", b, n), c.stream(stream))
+    dev, where = _device(), "apb_cache4_read"
+    n = problem.n_kv_heads * problem.bf16_rows * problem.head_dim
+    st = lib().apb_cache4_read(problem, _cache4(cache, dev, validate_cache4, problem, where),
+                               _rows4(k, "k", n, dev, validate_cache4, problem, where),
+                               _rows4(v, "v", n, dev, validate_cache4, problem, where),
+                               _stream4(stream, dev))
     if st:
-        _check(st, "apb_cache4_read")
+        _check(st, where)
 
 
 def validate_decode4(problem) -> int:
@@ -529,16 +534,28 @@ def decode4_attention(problem, q, cache: dict, o_part, lse_part, workspace, soft
     cache in 4 bits (``cache`` as in ``cache4_write``; may be None when cache_len
     is 0).  ``workspace`` is a device tensor of at least
     ``decode4_workspace_size`` bytes (any dtype)."""
-    c, t = _Call("apb_decode4_attention", validate_decode4, problem), _types()
-    if workspace is None or workspace.get_device() != c.dev or not workspace.is_contiguous():
-        _check(validate_decode4(problem), "apb_decode4_attention")
+    dev, where = _device(), "apb_decode4_attention"
+    if workspace is None or workspace.get_device() != dev or not workspace.is_contiguous():
+        _check(validate_decode4(problem), where)
         raise ValueError("workspace must be a contiguous device tensor, on the current device")
-    rows, d = problem.n_q_heads * problem.n_new, problem.head_dim
+    rows, f32 = problem.n_q_heads * problem.n_new, _Cuda.f32
+    n = rows * problem.head_dim
+    if not (o_part is not None and lse_part is not None
+            and o_part.dtype is f32 and lse_part.dtype is f32
+            and o_part.numel() == n and lse_part.numel() == rows
+            and o_part.get_device() == dev and lse_part.get_device() == dev
+            and o_part.is_contiguous() and lse_part.is_contiguous()):
+        status = validate_decode4(problem)
+        for t, name, size in ((o_part, "o_part", n), (lse_part, "lse_part", rows)):
+            if t is None:
+                _check(status or 1, where)
+            if not (t.dtype is f32 and t.numel() == size and t.get_device() == dev
+                    and t.is_contiguous()):
+                _wrong(t, name, (f32,), size, dev, status, where)
     st = lib().apb_decode4_attention(
-        problem, c.ptr(q, "q", t.bf16, rows * d),
-        None if cache is None else c.cache(cache, problem.n_kv_heads, problem.capacity, d),
-        c.ptr(o_part, "o_part", t.f32, rows * d), c.ptr(lse_part, "lse_part", t.f32, rows),
-        softmax_scale, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-        c.stream(stream))
+        problem, _rows4(q, "q", n, dev, validate_decode4, problem, where),
+        None if cache is None else _cache4(cache, dev, validate_decode4, problem, where),
+        o_part.data_ptr(), lse_part.data_ptr(), softmax_scale, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream4(stream, dev))
     if st:
-        _check(st, "apb_decode4_attention")
+        _check(st, where)

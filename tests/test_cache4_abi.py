@@ -176,6 +176,8 @@ def test_binding_checks_its_tensors():
     with pytest.raises(apb.ApbError) as e:
         apb.cache4_write(_rows(first_row=90), k, k, cache)
     assert e.value.status == 2
+    with pytest.raises(apb.ApbError, match="apb_cache4_read: APB_ERR_NULL_POINTER"):
+        apb.cache4_read(p, dict(cache, k_codes=None), k, k)
     with pytest.raises(ValueError, match="workspace"):
         apb.decode4_attention(_step(), k, cache, None, None, None)
     with pytest.raises(apb.ApbError):
