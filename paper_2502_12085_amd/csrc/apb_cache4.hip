@@ -16,6 +16,10 @@
 //
 // Both directions are bound by HBM: 2 bytes of bf16 and 17 / 32 of cache an element.
 // A thread takes 8 elements (16 bytes of bf16, 4 of codes), a group is four threads.
+// The bf16 side passes the caches by, which leaves them to the cache's codes.  131072 rows
+// of 8 heads of d = 128 (679 MB): write 121 -> 113 us (6.0 TB/s), read 121 -> 106 (6.4),
+// against four rows a thread and plain loads and stores; eight rows 128 and 127, one 114
+// and 130.  A few rows are one launch's latency, 2.4 us.
 #include "apb_internal.h"
 
 namespace apb {
@@ -26,7 +30,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
-constexpr int kSteps = 4;  // rows a thread moves, their loads in flight together
+constexpr int kSteps = 2;  // rows a thread moves, their loads in flight together
 
 constexpr int rows_per_block(int d) { return kThreads / (d / 8) * kSteps; }
 
@@ -74,7 +78,7 @@ __global__ void __launch_bounds__(kThreads) cache4_write_kernel(Cache4Args a) {
   for (int i = 0; i < kSteps; ++i) {
     const int r = p.row + i * STEP;
     x[i] = u32x4{};
-    if (r < a.n_rows) x[i] = *reinterpret_cast<const u32x4*>(src + (size_t)r * D);
+    if (r < a.n_rows) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (size_t)r * D));
   }
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
@@ -126,7 +130,7 @@ __global__ void __launch_bounds__(kThreads) cache4_read_kernel(Cache4Args a) {
     y[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], scale, 1));
     y[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], scale, 2));
     y[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], scale, 3));
-    if (r < a.n_rows) *reinterpret_cast<u32x4*>(dst + (size_t)r * D) = y;
+    if (r < a.n_rows) __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(dst + (size_t)r * D));
   }
 }
 
