@@ -160,6 +160,67 @@ def test_long_caches(shape):
           norm_bound=1e-5)
 
 
+@pytest.mark.parametrize("shape", [
+    # the forms that the shapes above leave out: one launch and splits of 32 rows, one
+    # split of many rows, and so many heads that a split of each fills the GPU
+    (4, 1, 64, 130, 128, 4, 1),       # 16 rows, four blocks
+    (8, 2, 128, 120, 100, 3, 1),
+    (4, 1, 64, 300, 300, 5, 1),       # 20 rows, ten blocks: one launch
+    (8, 1, 128, 300, 290, 4, 0),
+    (4, 1, 64, 100, 97, 7, 1),        # 28 rows, four blocks
+    (8, 1, 128, 100, 90, 3, 1),
+    (4, 1, 64, 2000, 1999, 7, 1),     # 28 rows, splits
+    (8, 1, 128, 2000, 1777, 4, 0),
+    (8, 2, 64, 100, 77, 15, 1),       # 60 rows, one split
+    (8, 2, 128, 128, 128, 11, 0),
+    (8, 2, 64, 120, 120, 40, 1),      # 160 rows, one split
+    (8, 2, 128, 100, 93, 33, 0),
+    (8, 2, 64, 1500, 1450, 15, 1),    # 60 rows, splits
+    (8, 2, 128, 1500, 1450, 15, 1),
+    (8, 2, 64, 30000, 29000, 1, 1),   # eight waves' splits
+    (300, 300, 64, 200, 199, 1, 1),   # one split each of more heads than CUs
+    (600, 300, 128, 200, 160, 9, 0),
+    (300, 300, 64, 200, 150, 35, 1),
+    (260, 260, 64, 140, 131, 70, 1),
+    (270, 90, 64, 400, 400, 30, 1),   # 90 heads: 270 row blocks
+    (3, 3, 128, 900, 900, 300, 1),    # an odd number of (split, head) pairs, three row blocks
+    (14, 7, 64, 500, 450, 100, 0),
+])
+def test_forms(shape):
+    need_gpu()
+    say(f"[decode4 forms] {shape}")
+    n_q, n_kv, d, cap, keys, n_new, causal = shape
+    q, cache = make(n_q, n_kv, d, cap, keys, n_new, seed=n_q + keys)
+    k, v = held(cache, keys)
+    got = run(q, cache, n_kv, cap, keys, causal)
+    check(f"decode4 {shape}", got, oracle.decode4_ref(q, k, v, causal=causal, bound=True), keys, d,
+          norm_bound=1e-5)
+
+
+def _random_shapes():
+    rng = np.random.default_rng(77)
+    out = []
+    for _ in range(40):
+        n_kv, g = int(rng.choice([1, 2, 3, 8])), int(rng.integers(1, 9))
+        d, causal = int(rng.choice([64, 128])), int(rng.integers(0, 2))
+        n_new = int(2 ** rng.uniform(0, 6.6))
+        keys = max(int(2 ** rng.uniform(0, 12)), n_new if causal else 1)
+        out.append((n_kv * g, n_kv, d, keys + int(rng.integers(0, 70)), keys, n_new, causal))
+    return out
+
+
+@pytest.mark.parametrize("shape", _random_shapes())
+def test_random_shapes(shape):
+    need_gpu()
+    say(f"[decode4 random] {shape}")
+    n_q, n_kv, d, cap, keys, n_new, causal = shape
+    q, cache = make(n_q, n_kv, d, cap, keys, n_new, seed=keys + n_new)
+    k, v = held(cache, keys)
+    got = run(q, cache, n_kv, cap, keys, causal)
+    check(f"decode4 {shape}", got, oracle.decode4_ref(q, k, v, causal=causal, bound=True), keys, d,
+          norm_bound=1e-5)
+
+
 # one or a few row blocks, many rows; each with a late key that dwarfs the others
 ROWS = [(4, 1, 64, 1), (8, 2, 128, 3), (8, 2, 128, 20), (4, 2, 64, 70), (4, 2, 128, 70)]
 
