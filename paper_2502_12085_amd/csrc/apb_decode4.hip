@@ -75,20 +75,16 @@ __device__ __forceinline__ f32x16 product(const bf16x8& a, const bf16x8& b, cons
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// Tiles of 32 keys in LDS, bf16 row by row, chunk (16 bytes) c of key r at chunk c ^ swz(r).
+// A V tile of 32 keys in LDS, bf16 row by row, chunk (16 bytes) c of key r at chunk c ^ swz(r).
 // A clock serves 16 lanes' 16 bytes or 32 lanes' transposing reads, on 64 banks (256 bytes,
 // one row of d = 128, two of 64).
-//  K: reads of one chunk of 16 keys; writes (16 lanes: chunks 4 g + j of some keys) of
-//  neighbouring keys.
-template <int D>
-__device__ __forceinline__ int k_swz(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
-//  V: transposing reads of 8 keys x 32 bytes (N = 16) or 4 keys x 64 bytes (N = 32).
+// Transposing reads take 8 keys x 32 bytes (N = 16) or 4 keys x 64 bytes (N = 32).
 template <int D, int N>
 __device__ __forceinline__ int v_swz(int r) {
   if (N == 16) return (D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3)) ^ ((r >> 3) & 1);
   return (D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1)) ^ ((r >> 2) & 3);
 }
-// Writes of V go without conflicts where 16 lanes' keys differ in the bits of r that move
+// Its writes go without conflicts where 16 lanes' keys differ in the bits of r that move
 // their chunks j: key x of 32 (the group's lanes neighbours, then keys in this order).
 template <int D, int N>
 __device__ __forceinline__ int v_key(int x) {
@@ -101,10 +97,9 @@ __device__ __forceinline__ int v_key(int x) {
 }
 
 // A group's 32 elements into its row's four chunks at `at` (exclusive or 16 j).  A group
-// of NaN goes there as zeros where it is V's: in a product a zero probability would not
-// keep it out.
-__device__ __forceinline__ void put_group(uint32_t at, const u32x4& codes, unsigned b, bool v) {
-  const bool bad = v && b == 255;
+// of NaN goes there as zeros: in a product a zero probability would not keep it out.
+__device__ __forceinline__ void put_group(uint32_t at, const u32x4& codes, unsigned b) {
+  const bool bad = b == 255;
   const float scale = __uint_as_float(bad ? 0u : b << 23);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -200,28 +195,23 @@ struct Rows4 {
       }
   }
 
-  // Logits of SUB blocks to probabilities, in their three parts as P operands, and the
-  // running maximum and sum.  All of them against one maximum: O is rescaled when that
-  // rises, and their values are not in it yet.
-  template <int SUB>
-  __device__ __forceinline__ void softmax(const Acc (&s)[SUB][TILES], float scale,
-                                          u32x4 (&pr)[SUB][PS][3]) {
-    constexpr int M = NS * SUB;
-    float e[M], sum;
-    auto at = [&](int i) __attribute__((always_inline)) { return logit(s[i / NS], i % NS); };
+  // Logits of a block to probabilities, in their three parts as P operands, and the
+  // running maximum and sum.
+  __device__ __forceinline__ void softmax(const Acc (&s)[TILES], float scale, u32x4 (&pr)[PS][3]) {
+    float e[NS], sum;
     auto exps = [&]() __attribute__((always_inline)) {
       sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < M; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(at(i), scale, -m_run));
+      for (int i = 0; i < NS; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(logit(s, i), scale, -m_run));
 #pragma unroll
-      for (int i = 0; i < M; i += 8)
+      for (int i = 0; i < NS; i += 8)
         sum += ((e[i] + e[i + 1]) + (e[i + 2] + e[i + 3])) + ((e[i + 4] + e[i + 5]) + (e[i + 6] + e[i + 7]));
     };
     exps();
     if (__any(!(sum <= kSumLimit))) {
-      float mx = at(0);
+      float mx = logit(s, 0);
 #pragma unroll
-      for (int i = 1; i < M; ++i) mx = fmaxf(mx, at(i));
+      for (int i = 1; i < NS; ++i) mx = fmaxf(mx, logit(s, i));
 #pragma unroll
       for (int off = N; off < 64; off *= 2) mx = fmaxf(mx, __shfl_xor(mx, off));
       const float m_new = fmaxf(m_run, mx * scale);
@@ -229,8 +219,8 @@ struct Rows4 {
         // nothing but keys that the row does not see, and NaN, which stays
         sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < M; ++i) {
-          const float y = at(i);
+        for (int i = 0; i < NS; ++i) {
+          const float y = logit(s, i);
           e[i] = y == -INFINITY ? 0.f : y;
           sum += e[i];
         }
@@ -245,7 +235,7 @@ struct Rows4 {
     }
     l_run += sum;
 #pragma unroll
-    for (int i = 0; i < M / 2; ++i) {
+    for (int i = 0; i < NS / 2; ++i) {
       unsigned hi[2], mid[2], lo[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -254,7 +244,7 @@ struct Rows4 {
         mid[t] = __float_as_uint(r1);
         lo[t] = __float_as_uint(r1 - __uint_as_float(mid[t] & 0xFFFF0000u));
       }
-      u32x4(&out)[3] = pr[2 * i / NS][2 * i % NS / 8];
+      u32x4(&out)[3] = pr[i / 4];
       out[0][i & 3] = __builtin_amdgcn_perm(hi[1], hi[0], 0x07060302u);
       out[1][i & 3] = __builtin_amdgcn_perm(mid[1], mid[0], 0x07060302u);
       out[2][i & 3] = __builtin_amdgcn_perm(lo[1], lo[0], 0x07060302u);
@@ -355,7 +345,7 @@ struct Rows4 {
   }
 };
 
-// Up to 32 rows of a KV head: WK waves, each with 32-key blocks of its own.  A product
+// N rows of a KV head: WK waves, each with 32-key blocks of its own.  A product
 // over the head size may take it in any order that both operands share, so a lane takes
 // the part of its key that lies together and K goes from memory to the operand
 // registers without LDS; a wave has its V tile to itself, so that the loop has no barrier.
@@ -437,13 +427,13 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
   // waves of a CU have 35 KiB under way.
   auto block = [&](Block& x, int b) __attribute__((always_inline)) {
     const int c0 = 32 * b;
-    typename Rows::Acc s[1][Rows::TILES];
+    typename Rows::Acc s[Rows::TILES];
 #pragma unroll
     for (int i = 0; i < Rows::TILES; ++i)
 #pragma unroll
       for (int j = 0; j < KW; ++j) {
         const float scale = __uint_as_float(x.kb[i][j / 4 % KB] << 23);  // b = 255: NaN elements
-        rows.logits(s[0][i], as_bf16(elements(x.kw[i][j], scale)), j);
+        rows.logits(s[i], as_bf16(elements(x.kw[i][j], scale)), j);
       }
 
     // V -> LDS; a group of NaN goes into O by hand, for the rows that see it: the first
@@ -452,7 +442,7 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
     bool bad = false;
 #pragma unroll
     for (int v = 0; v < VL; ++v) {
-      put_group(v_put[v], x.vw[v], x.vb[v], true);
+      put_group(v_put[v], x.vw[v], x.vb[v]);
       bad |= x.vb[v] == 255;
     }
     const bool any_bad = __any(bad);
@@ -476,15 +466,15 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
       for (int ps = 0; ps < Rows::PS; ++ps) v[db][ps] = Rows::v_operand(v_get, db, ps);
     __builtin_amdgcn_sched_barrier(0);
 
-    if (c0 + 32 > vis_all) rows.mask(s[0], c0);
-    u32x4 pr[1][Rows::PS][3];
+    if (c0 + 32 > vis_all) rows.mask(s, c0);
+    u32x4 pr[Rows::PS][3];
     rows.softmax(s, p.scale_log2, pr);
 #pragma unroll
     for (int ps = 0; ps < Rows::PS; ++ps)
 #pragma unroll
       for (int t = 0; t < 3; ++t)
 #pragma unroll
-        for (int db = 0; db < Rows::NDB; ++db) rows.values(db, v[db][ps], pr[0][ps][t]);
+        for (int db = 0; db < Rows::NDB; ++db) rows.values(db, v[db][ps], pr[ps][t]);
     if (any_bad) {
 #pragma unroll
       for (int n = 0; n < G; ++n)
@@ -496,193 +486,6 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
     for (int b = b0 + wave; b < b1; b += WK) block(x, b);
   }
   rows.template finish<WK, WHOLE>(p, at, row0, wave, lds, ml_lds);
-}
-
-// More rows: eight waves, WR of them with 32 rows each and WK = 8 / WR such sets, which
-// share a split's keys.  A step is 128 keys: all threads make its codes bf16 and put K
-// and V into LDS, where each set reads 128 / WK of them, so that the work of a conversion
-// is shared by 32 * WR rows.
-// Two buffers, one barrier a step.  The waves of a SIMD are half a step apart, so that
-// the products of one go with the vector work of the other: group A (waves 0 .. 3) passes
-// the barrier before its products, group B after them.  Between two barriers
-//   A: S(t) = Q K(t) and O += P(t-1) V(t-1), then softmax(t), K(t+1) and V(t) -> LDS
-//   B: softmax(t-1), K(t+1) and V(t) -> LDS, then S(t) and O += P(t-1) V(t-1)
-// read K(t) and V(t-1) and write K(t+1) and V(t); the codes of the next writes are in
-// flight meanwhile.  What bounds it is the SIMDs' vector issue: a 32-key block of 32
-// rows is 32 products of 8 cycles, 150 instructions of 4.7, 16 exponentials of 16 and 16
-// conversions of 8 a wave.  (With 16x16x32 products, 64 of them, 128 tokens over 16385
-// keys took 70.5 us; products and softmax of neighbouring blocks interleaved in one
-// wave, 16x16x32: 79.0.)
-template <int D, int WR, bool WHOLE>
-__global__ void __launch_bounds__(512, 2) decode4_shared_kernel(Dec4Params p) {
-  constexpr int N = 32, WK = 8 / WR, SUB = 4 / WK;  // 32-key blocks of a step and set
-  using Rows = Rows4<D, N>;
-  constexpr int G = D / 32, TILE = 32 * D * 2;
-  __shared__ __attribute__((aligned(256))) uint8_t lds[2][2][4][TILE];  // K or V, buffer, block
-  static_assert(sizeof(lds) == 8 * Rows::OUT, "O of eight waves at the end");
-  __shared__ float ml_lds[WR][2][WK][N];
-  // First key (of 32) whose values of a group are NaN, and whether there is one, by step % 3:
-  // cleared in the step before it is set, read in the one after.
-  __shared__ int nan_lds[3][4][4], any_lds[3];
-
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
-  const bool group_b = wave >= 4;
-  const Place4 at = place4(p.n_split, p.n_rb, p.n_kv);
-  const int nblk = (p.Lc + 31) / 32;
-  const int b0 = at.split * p.blocks_per_split, b1 = min(b0 + p.blocks_per_split, nblk);
-  const int steps = (b1 - b0 + 3) / 4;
-  const int vis_all = min(p.causal ? p.Lc - p.n_new + 1 : p.Lc, 32 * b1);
-
-  // This thread's groups of a step: (key, g) of K and of V (d = 128), or of one of them by
-  // wave (d = 64).  Every load and write is made, whatever the step: past the split's end
-  // they repeat its last key and go where nothing is read any more.  (Where some are
-  // left out, the compiler waits for all that are in flight before the first is used.)
-  constexpr int NU = D / 64;
-  const int unit = NU == 2 ? tid : (tid & 63) + (tid >> 7) * 64, g = unit % G;
-  const uint32_t base = lds_base(lds);
-  constexpr uint32_t BUF = 4 * TILE, V = 2 * BUF;
-  bool is_v[NU];
-  int key[NU];
-  uint32_t put_at[NU];
-#pragma unroll
-  for (int u = 0; u < NU; ++u) {
-    is_v[u] = NU == 2 ? u == 1 : (wave & 1) != 0;
-    key[u] = is_v[u] ? v_key<D, N>(unit / G) : unit / G;
-    const int swz = is_v[u] ? v_swz<D, N>(key[u]) : k_swz<D>(key[u]);
-    put_at[u] = base + (is_v[u] ? V : 0) + (uint32_t)(key[u] * 2 * D) + 16u * ((4 * g) ^ swz);
-  }
-
-  struct Unit {
-    u32x4 w;
-    unsigned b;
-  };
-  // The codes of K(step) and V(step - 1), and their way into LDS.
-  auto load = [&](int step, Unit (&x)[NU]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      const int c0 = min(32 * (b0 + 4 * max(step - (is_v[u] ? 1 : 0), 0)), p.Lc - 1);
-      const uint32_t k = (uint32_t)min(key[u], p.Lc - 1 - c0);
-      const size_t r0 = (size_t)at.kvh * p.capacity + c0;
-      const uint8_t* codes = (is_v[u] ? p.v_codes : p.k_codes) + r0 * (D / 2);
-      const uint8_t* scales = (is_v[u] ? p.v_scales : p.k_scales) + r0 * G;
-      x[u].w = *reinterpret_cast<const u32x4*>(codes + (k * (D / 2) + 16u * g));
-      x[u].b = scales[k * G + g];
-    }
-  };
-  auto put = [&](int step, const Unit (&x)[NU]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      const int of = step - (is_v[u] ? 1 : 0);
-      put_group(put_at[u] + (of & 1 ? BUF : 0), x[u].w, x[u].b, is_v[u]);
-      if (is_v[u] && x[u].b == 255 && of < steps) {
-        atomicMin(&nan_lds[of % 3][key[u] / 32][g], key[u] % 32);
-        any_lds[of % 3] = 1;
-      }
-    }
-  };
-  auto put_keys = [&](const Unit (&x)[NU]) __attribute__((always_inline)) {  // K(0)
-#pragma unroll
-    for (int u = 0; u < NU; ++u)
-      if (!is_v[u]) put_group(put_at[u], x[u].w, x[u].b, false);
-  };
-  auto clear = [&](int step) __attribute__((always_inline)) {  // by group B
-    if (tid >= 256 && tid < 272) nan_lds[step % 3][(tid & 15) / 4][tid & 3] = 32;
-    if (tid == 272) any_lds[step % 3] = 0;
-  };
-
-  Rows rows;
-  const int row0 = N * (WR * at.row_block + wr);
-  Unit codes[NU], first[NU];
-  if (steps > 0) {
-    load(0, first);
-    load(1, codes);
-  }
-  rows.start(p, at.kvh, row0, [&](int j) { return 16 * j + 8 * Rows::group(); });
-  rows.vis = min(rows.vis, 32 * b1);
-  const int kr = lane & 31;  // K operand of product j: chunk 2 j + lane / 32 of key kr
-  const uint32_t k_get = base + (uint32_t)(kr * 2 * D) + 16u * ((lane >> 5) ^ k_swz<D>(kr)) + wk * SUB * TILE;
-  const uint32_t v_get = Rows::v_lane(base + V + wk * SUB * TILE);
-
-  clear(0);
-  if (steps > 0) put_keys(first);
-  __syncthreads();
-  if (group_b && steps > 0) {
-    put(1, codes);
-    load(2, codes);
-    clear(1);
-  }
-  typename Rows::Acc s[SUB][1];
-  u32x4 pr[SUB][Rows::PS][3];
-  // The products, in turns of two dim blocks of O with one P operand (six) and two of S;
-  // a turn's operands are read while the one before it goes on.
-  auto products = [&](int step, auto with_s, auto with_o) __attribute__((always_inline)) {
-    constexpr bool S = decltype(with_s)::value, O = decltype(with_o)::value;
-    constexpr int TURNS = Rows::KS / 2;  // of a block
-    static_assert(Rows::NDB * Rows::PS == 2 * TURNS && Rows::PS == 2, "as many turns for O");
-    const uint32_t kt = k_get + (step & 1 ? BUF : 0), vt = v_get + (step & 1 ? 0 : BUF);
-    bf16x8 k[2][2], v[2][2];
-    auto read = [&](int n) __attribute__((always_inline)) {
-      const int t = n / TURNS, m = n % TURNS;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if constexpr (O) v[n & 1][i] = Rows::v_operand(vt + t * TILE, m / 2 * 2 + i, m % 2);
-        if constexpr (S)
-          k[n & 1][i] = as_bf16(*(lds_u32x4*)(uintptr_t)((kt ^ (32u * (2 * m + i))) + (uint32_t)(t * TILE)));
-      }
-    };
-    read(0);
-#pragma unroll
-    for (int n = 0; n < TURNS * SUB; ++n) {
-      const int t = n / TURNS, m = n % TURNS;
-      if (n + 1 < TURNS * SUB) read(n + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int u = 0; u < 3; ++u) {
-        if constexpr (O) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) rows.values(m / 2 * 2 + i, v[n & 1][i], pr[t][m % 2][u]);
-        }
-        if constexpr (S) {
-          if (u < 2) rows.logits(s[t][0], k[n & 1][u], 2 * m + u);
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  auto not_numbers = [&](int step, int any) __attribute__((always_inline)) {
-    if (any == 0) return;
-    for (int t = 0; t < SUB; ++t)
-      for (int n = 0; n < G; ++n) {
-        const int blk = wk * SUB + t, f = nan_lds[step % 3][blk][n];
-        if (f < 32) rows.not_a_number(n, 32 * (b0 + 4 * step + blk) + f);
-      }
-  };
-  auto turn = [&](int step, auto more) __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < SUB; ++t) {
-      const int c0 = 32 * (b0 + 4 * step + wk * SUB + t);
-      if (c0 + 32 > vis_all) rows.mask(s[t], c0);
-    }
-    rows.softmax(s, p.scale_log2, pr);
-    put(step + (group_b ? 2 : 1), codes);
-    load(step + (group_b ? 3 : 2), codes);
-    if (group_b) clear(step + 2);
-    if (!group_b) __syncthreads();
-    const int any = any_lds[step % 3];
-    __builtin_amdgcn_s_setprio(1);
-    products(step + 1, more, std::true_type{});
-    __builtin_amdgcn_s_setprio(0);
-    not_numbers(step, any);
-    if (decltype(more)::value && group_b) __syncthreads();
-  };
-  if (steps > 0) {
-    products(0, std::true_type{}, std::false_type{});
-    if (group_b) __syncthreads();
-    for (int step = 0; step + 1 < steps; ++step) turn(step, std::true_type{});
-    turn(steps - 1, std::false_type{});
-  }
-  rows.template finish<WK, WHOLE>(p, at, row0, wk, &lds[0][0][0][0] + wr * WK * Rows::OUT, ml_lds[wr]);
 }
 
 // The splits of a row: O = sum_s 2^(m_s - m) O_s / l, l = sum_s 2^(m_s - m) l_s, with m
@@ -752,20 +555,18 @@ __global__ void __launch_bounds__(kMergeThreads) decode4_merge_kernel(
   if (tid == 0) lse[row] = l == 0.f ? -INFINITY : 0.69314718055994531f * (m + log2f(l));
 }
 
+template <int D, int N, bool WHOLE>
+void launch_rows(const Dec4Params& p, const Decode4Plan& pl, dim3 grid, hipStream_t stream) {
+  if (pl.waves == 8)
+    hipLaunchKernelGGL((decode4_kernel<D, N, 8, WHOLE>), grid, dim3(512), 0, stream, p);
+  else
+    hipLaunchKernelGGL((decode4_kernel<D, N, 4, WHOLE>), grid, dim3(256), 0, stream, p);
+}
+
 template <int D, bool WHOLE>
 void launch_splits(const Dec4Params& p, const Decode4Plan& pl, dim3 grid, hipStream_t stream) {
-  if (pl.rows == 16 && pl.waves == 8)
-    hipLaunchKernelGGL((decode4_kernel<D, 16, 8, WHOLE>), grid, dim3(512), 0, stream, p);
-  else if (pl.rows == 16)
-    hipLaunchKernelGGL((decode4_kernel<D, 16, 4, WHOLE>), grid, dim3(256), 0, stream, p);
-  else if (pl.rows == 32 && WHOLE && pl.waves == 8)  // (splits of 32 rows have four)
-    hipLaunchKernelGGL((decode4_kernel<D, 32, 8, true>), grid, dim3(512), 0, stream, p);
-  else if (pl.rows == 32)
-    hipLaunchKernelGGL((decode4_kernel<D, 32, 4, WHOLE>), grid, dim3(256), 0, stream, p);
-  else if (pl.rows == 64)
-    hipLaunchKernelGGL((decode4_shared_kernel<D, 2, WHOLE>), grid, dim3(512), 0, stream, p);
-  else
-    hipLaunchKernelGGL((decode4_shared_kernel<D, 4, WHOLE>), grid, dim3(512), 0, stream, p);
+  if (pl.rows == 16) launch_rows<D, 16, WHOLE>(p, pl, grid, stream);
+  else launch_rows<D, 32, WHOLE>(p, pl, grid, stream);
 }
 
 template <int D>

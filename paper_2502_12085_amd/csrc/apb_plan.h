@@ -156,9 +156,8 @@ inline DecodePlan plan_decode(int64_t n_q, int64_t n_kv, int head_dim, int64_t c
 struct Decode4Plan {
   int n_split;
   int blocks_per_split;  // 32-key blocks
-  int rows;              // rows of a KV head per workgroup: 16 or 32 (its waves have
-                         // blocks of their own), 64 or 128 (they share steps of four)
-  int waves;             // of a workgroup
+  int rows;              // rows of a KV head per workgroup (16 or 32)
+  int waves;             // of a workgroup, which share its blocks (4 or 8)
   int row_blocks;        // workgroups along the rows of a KV head
   uint64_t workspace_bytes;
 };
@@ -174,28 +173,47 @@ inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t
                                 int64_t n_new) {
   Decode4Plan pl;
   const int64_t R = n_q / n_kv * n_new, nblk = (cache_len + 31) / 32;
-  pl.rows = R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128;
-  const int64_t row_blocks = (R + pl.rows - 1) / pl.rows;
-  const int64_t per_cu = kCus / (n_kv * row_blocks);  // splits that give every CU a workgroup
-  int64_t n_split;
-  pl.waves = pl.rows > 32 ? 8 : 4;
-  if (pl.rows <= 32 && nblk <= decode4_one_launch_blocks(pl.rows)) {
-    n_split = 1;
+  pl.rows = R <= 16 ? 16 : 32;
+  const int64_t row_blocks = (R + pl.rows - 1) / pl.rows, base = n_kv * row_blocks;
+  const int64_t most = std::max<int64_t>((nblk + 3) / 4, 1);  // a block for each of four waves
+  int64_t n_split = 1;
+  pl.waves = 4;
+  if (nblk <= decode4_one_launch_blocks(pl.rows)) {
     if (nblk > 4) pl.waves = 8;
-  } else if (pl.rows == 16 && nblk >= 4 * per_cu && per_cu > 0) {
-    // eight waves with a block each in half a round at least: as many waves on a CU as
-    // two workgroups of four, and half the partials (8 heads: 16385 keys 12.3 -> 11.6
-    // us, 4097 8.7 -> 8.5; 2048 7.4 against 8.3)
-    pl.waves = 8;
-    n_split = per_cu;
+  } else if (pl.rows == 16) {
+    // Two workgroups of four waves a CU; or one of eight, which have a block each in half a
+    // round at least: as many waves, half the partials (8 heads: 16385 keys 12.3 -> 11.6
+    // us, 4097 8.7 -> 8.5; 2048 7.4 against 8.3).
+    const int64_t per_cu = kCus / base;
+    if (per_cu > 0 && nblk >= 4 * per_cu) {
+      pl.waves = 8;
+      n_split = per_cu;
+    } else {
+      n_split = std::max<int64_t>(std::min(2 * per_cu, most), 1);
+    }
   } else {
-    n_split = std::min<int64_t>(pl.rows == 16 ? 2 * per_cu : per_cu, (nblk + 3) / 4);
+    // The splits that make one, two, .. rounds of a workgroup a CU, by what they cost in
+    // blocks of eight waves (1.75 us): a workgroup's own blocks, its start and end (3), and
+    // the partials (1.5 and their bytes).  320 row blocks of 250 key blocks (40 / 8 heads,
+    // 256 tokens) 114 us in one split, 101 so.
+    double best = 0;
+    for (int64_t r = 1; r <= 6; ++r) {
+      const int64_t n = std::max<int64_t>(std::min(kCus * r / base, most), 1);
+      const double rounds = (double)((base * n + kCus - 1) / kCus);
+      const double partials = (double)n * (double)(n_q * n_new) * (head_dim + 2) * 8;  // there and back
+      const double cost = rounds * ((double)((nblk + 8 * n - 1) / (8 * n)) + 3.0) +
+                          (n > 1 ? 1.5 + partials / 7.9e6 : 0.0);
+      if (r == 1 || cost < best) {
+        best = cost;
+        n_split = n;
+      }
+    }
+    // one round of eight waves where they have three blocks each (256 rows of 8 heads x
+    // 16448 keys 43.5 -> 40.8 us, x 4000 18.6 -> 18.1; 40 rows x 4000 11.1 against 12.0),
+    // else of four, two workgroups a CU where there are as many
+    if (base * n_split <= kCus && nblk >= 24 * n_split) pl.waves = 8;
   }
-  n_split = std::max<int64_t>(n_split, 1);
-  int64_t bps = std::max<int64_t>((nblk + n_split - 1) / n_split, 1);
-  // whole steps: a part of one takes as long (256 rows: 16448 keys 50.4 -> 47.7 us, 2049
-  // 25.6 -> 22.7)
-  if (pl.rows > 32) bps = (bps + 3) / 4 * 4;
+  const int64_t bps = std::max<int64_t>((nblk + n_split - 1) / n_split, 1);
   n_split = std::max<int64_t>((nblk + bps - 1) / bps, 1);
   pl.n_split = (int)n_split;
   pl.blocks_per_split = (int)bps;

@@ -161,8 +161,8 @@ def test_long_caches(shape):
 
 
 @pytest.mark.parametrize("shape", [
-    # the forms that the shapes above leave out: one launch and splits of 32 rows, one
-    # split of many rows, and so many heads that a split of each fills the GPU
+    # the forms that the shapes above leave out: one launch, one split of many rows, so
+    # many heads that a split of each fills the GPU, splits of several rounds
     (4, 1, 64, 130, 128, 4, 1),       # 16 rows, four blocks
     (8, 2, 128, 120, 100, 3, 1),
     (4, 1, 64, 300, 300, 5, 1),       # 20 rows, ten blocks: one launch
@@ -177,13 +177,20 @@ def test_long_caches(shape):
     (8, 2, 128, 100, 93, 33, 0),
     (8, 2, 64, 1500, 1450, 15, 1),    # 60 rows, splits
     (8, 2, 128, 1500, 1450, 15, 1),
-    (8, 2, 64, 30000, 29000, 1, 1),   # eight waves' splits
+    (8, 2, 64, 30000, 29000, 1, 1),   # splits of eight waves
+    (8, 1, 64, 50000, 49000, 5, 1),
+    (8, 1, 128, 50000, 49000, 5, 0),
+    (16, 8, 64, 8000, 7777, 66, 1),
+    (16, 8, 128, 8000, 7777, 66, 1),
     (300, 300, 64, 200, 199, 1, 1),   # one split each of more heads than CUs
     (600, 300, 128, 200, 160, 9, 0),
     (300, 300, 64, 200, 150, 35, 1),
     (260, 260, 64, 140, 131, 70, 1),
     (270, 90, 64, 400, 400, 30, 1),   # 90 heads: 270 row blocks
-    (3, 3, 128, 900, 900, 300, 1),    # an odd number of (split, head) pairs, three row blocks
+    (3, 3, 128, 900, 900, 300, 1),    # ten row blocks, of heads and splits off 8
+    (200, 100, 64, 1700, 1650, 17, 1),  # 200 row blocks: splits of more than one round
+    (128, 128, 128, 700, 650, 40, 1),
+    (16, 16, 128, 900, 850, 200, 0),
     (14, 7, 64, 500, 450, 100, 0),
 ])
 def test_forms(shape):
