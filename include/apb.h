@@ -30,7 +30,8 @@
  * cache held in 4 bits, a quarter of the bytes:
  *   apb_cache4_write     quantise K and V rows into the cache;
  *   apb_cache4_read      read rows of it back in bf16;
- *   apb_decode4_attention  one host's attention of the new tokens over it.
+ *   apb_decode4_attention  one host's exact attention of the new tokens over it,
+ *                        with the LSE.
  *
  * Conventions shared by every entry point
  *   - All tensor pointers are caller-owned DEVICE memory on the current HIP
@@ -300,7 +301,7 @@ apb_status_t apb_merge_partials(int32_t n_parts, int32_t rows, int32_t head_dim,
  * ------------------------------------------------------------------------ */
 typedef struct {
   uint8_t* k_codes;   /* [n_kv][capacity][d / 2]   16-byte aligned            */
-  uint8_t* k_scales;  /* [n_kv][capacity][d / 32]  4-byte aligned             */
+  uint8_t* k_scales;  /* [n_kv][capacity][d / 32]  any alignment              */
   uint8_t* v_codes;   /* as k_codes                                           */
   uint8_t* v_scales;  /* as k_scales                                          */
 } apb_cache4_t;
@@ -313,7 +314,9 @@ typedef struct {
   int32_t head_dim;   /* d, in {64, 128}                                      */
   int32_t capacity;   /* 1 .. 2^30 rows per head of the cache                 */
   int32_t first_row;  /* >= 0: first cache row                                */
-  int32_t n_rows;     /* >= 0: rows; first_row + n_rows <= capacity           */
+  int32_t n_rows;     /* >= 0: rows; first_row + n_rows <= capacity; fewer than
+                         2^23 blocks of 4096 elements, of whole rows of a head:
+                         n_kv * ceil(n_rows / (4096 / d)) < 2^23              */
   int32_t bf16_rows;  /* 0 .. 2^30 rows per head of the bf16 tensors          */
   int32_t bf16_first; /* >= 0: their first row; + n_rows <= bf16_rows         */
 } apb_cache4_problem_t;
@@ -357,7 +360,7 @@ typedef struct {
   int32_t head_dim;   /* d, in {64, 128}                                     */
   int32_t capacity;   /* 1 .. 2^30 rows per head that the cache has room for */
   int32_t cache_len;  /* 0 <= Lc <= capacity: the rows that hold keys        */
-  int32_t n_new;      /* >= 1 new tokens                                     */
+  int32_t n_new;      /* >= 1 new tokens; n_q * n_new < 2^24                 */
   int32_t causal;     /* 1 on the last host, whose cache already ends with the
                          new tokens' own rows (Lc >= n_new): new token j sees
                          rows 0 .. Lc - n_new + j; 0: every row of Lc        */
@@ -389,9 +392,10 @@ apb_status_t apb_decode4_workspace_size(const apb_decode4_problem_t* p, uint64_t
  *                   call overwrites it (calls that overlap in time must not
  *                   share one).  The library allocates nothing.
  * Arithmetic: bf16 queries against the cache's exact values, fp32 dot products
- * and softmax, fp32 accumulation and output.  A NaN among a row's visible logits
- * makes its o and lse NaN; a NaN group of a visible V row makes its 32 output
- * elements NaN.
+ * and softmax, no rounding of the probabilities, fp32 accumulation and output.  A
+ * NaN among a row's visible logits makes its o and lse NaN; a NaN group of a visible
+ * V row makes its 32 output elements NaN.  A logit that overflows to -inf is a key
+ * without weight, one of +inf or NaN is a NaN.
  */
 apb_status_t apb_decode4_attention(const apb_decode4_problem_t* p, const uint16_t* q,
                                    const apb_cache4_t* cache, float* o_part, float* lse_part,

@@ -485,6 +485,9 @@ apb_status_t apb_decode_attention_noalloc(const apb_decode_problem_t* p, const u
   return APB_OK;
 }
 
+// Workgroups of 256 threads that a launch has fewer than: its threads stay below 2^32.
+constexpr int64_t kMaxGrid256 = int64_t(1) << 24;
+
 apb_status_t apb_validate_cache4(const apb_cache4_problem_t* p) {
   if (!p) return APB_ERR_NULL_POINTER;
   if (p->n_kv_heads < 1 || p->n_kv_heads > 65536 || p->head_dim < 1) return APB_ERR_BAD_SHAPE;
@@ -496,7 +499,7 @@ apb_status_t apb_validate_cache4(const apb_cache4_problem_t* p) {
   if (p->head_dim != 64 && p->head_dim != 128) return APB_ERR_UNSUPPORTED;
   apb::Cache4Args a{};
   a.n_kv = p->n_kv_heads; a.head_dim = p->head_dim; a.n_rows = p->n_rows;
-  if (apb::cache4_blocks(a) >= (int64_t(1) << 31)) return APB_ERR_BAD_SHAPE;
+  if (apb::cache4_blocks(a) >= kMaxGrid256) return APB_ERR_BAD_SHAPE;
   return APB_OK;
 }
 
@@ -513,7 +516,7 @@ static apb_status_t cache4_checks(const apb_cache4_problem_t* p, const apb_cache
   if (!cache->k_codes || !cache->k_scales || !cache->v_codes || !cache->v_scales)
     return APB_ERR_NULL_POINTER;
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(cache->k_codes, 16) ||
-      !aligned(cache->v_codes, 16) || !aligned(cache->k_scales, 4) || !aligned(cache->v_scales, 4))
+      !aligned(cache->v_codes, 16))
     return APB_ERR_MISALIGNED;
   // whole tensors: all six lie apart, but that a write may take K and V from the
   // same memory
@@ -574,8 +577,8 @@ apb_status_t apb_validate_decode4(const apb_decode4_problem_t* p) {
   if (p->capacity < 1 || p->capacity > kMaxRows) return APB_ERR_BAD_SHAPE;
   if (p->cache_len < 0 || p->cache_len > p->capacity) return APB_ERR_BAD_SHAPE;
   if (p->causal == 1 && p->cache_len < p->n_new) return APB_ERR_BAD_SHAPE;
-  // rows of one GQA group and of the whole call stay well inside int32
-  if ((int64_t)p->n_q_heads * p->n_new > kMaxRows) return APB_ERR_BAD_SHAPE;
+  // the merge takes a workgroup a row
+  if ((int64_t)p->n_q_heads * p->n_new >= kMaxGrid256) return APB_ERR_BAD_SHAPE;
   if (p->head_dim != 64 && p->head_dim != 128) return APB_ERR_UNSUPPORTED;
   return APB_OK;
 }
@@ -608,8 +611,7 @@ apb_status_t apb_decode4_attention(const apb_decode4_problem_t* p, const uint16_
     return APB_ERR_NULL_POINTER;
   if (!aligned(q, 16) || !aligned(o_part, 16) || !aligned(lse_part, 4) || !aligned(workspace, 16))
     return APB_ERR_MISALIGNED;
-  if (has_cache && (!aligned(cache->k_codes, 16) || !aligned(cache->v_codes, 16) ||
-                    !aligned(cache->k_scales, 4) || !aligned(cache->v_scales, 4)))
+  if (has_cache && (!aligned(cache->k_codes, 16) || !aligned(cache->v_codes, 16)))
     return APB_ERR_MISALIGNED;
   apb::Decode4Args a = decode4_args(p);
   const uint64_t need = apb::decode4_workspace_bytes(a);

@@ -152,7 +152,7 @@ inline DecodePlan plan_decode(int64_t n_q, int64_t n_kv, int head_dim, int64_t c
 }
 
 // How a decode call over a 4-bit cache goes about it.  The workspace holds a partial
-// per split and row: fp32 O, maximum and sum.
+// per row and split, where there are several: fp32 O, maximum and sum.
 struct Decode4Plan {
   int n_split;
   int blocks_per_split;  // 32-key blocks
@@ -218,7 +218,9 @@ inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t
   pl.n_split = (int)n_split;
   pl.blocks_per_split = (int)bps;
   pl.row_blocks = (int)row_blocks;
-  pl.workspace_bytes = (uint64_t)n_split * (uint64_t)(n_q * n_new) * (uint64_t)(head_dim + 2) * 4;
+  // (one split writes the result itself; 16 bytes are the least that a caller passes)
+  pl.workspace_bytes =
+      n_split > 1 ? (uint64_t)n_split * (uint64_t)(n_q * n_new) * (uint64_t)(head_dim + 2) * 4 : 16;
   return pl;
 }
 

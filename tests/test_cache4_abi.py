@@ -49,7 +49,11 @@ def _step(**kw):
     (dict(head_dim=0), 2),
     (dict(head_dim=96), 3),
     (dict(head_dim=256), 3),
-    # more workgroups than a launch can have
+    # more threads than a launch can have: 64 rows of d = 64 a workgroup, K and V
+    (dict(n_kv_heads=1 << 13, capacity=1 << 17, n_rows=1 << 16, first_row=0, bf16_rows=1 << 17,
+          bf16_first=0), 2),
+    (dict(n_kv_heads=(1 << 13) - 1, capacity=1 << 17, n_rows=1 << 16, first_row=0,
+          bf16_rows=1 << 17, bf16_first=0), 0),
     (dict(n_kv_heads=65536, capacity=1 << 30, n_rows=1 << 30, first_row=0, bf16_rows=1 << 30,
           bf16_first=0), 2),
 ])
@@ -74,6 +78,8 @@ def test_validate_cache4(kw, code):
     (dict(n_kv_heads=0), 2),
     (dict(n_q_heads=65537, n_kv_heads=65537), 2),
     (dict(n_new=1 << 28, causal=0), 2),
+    (dict(n_new=1 << 21, causal=0), 2),      # more rows than a launch can have
+    (dict(n_new=(1 << 21) - 1, causal=0), 0),
     (dict(capacity=0, cache_len=0, causal=0), 2),
     (dict(capacity=(1 << 30) + 1), 2),
     (dict(head_dim=0), 2),
@@ -114,8 +120,6 @@ def test_rows_error_paths(write):
     assert call(v=V + 2) == 4
     assert call(cache=_cache(kc=KC + 8)) == 4
     assert call(cache=_cache(vc=VC + 4)) == 4
-    assert call(cache=_cache(ks=KS + 2)) == 4
-    assert call(cache=_cache(vs=VS + 1)) == 4
     # 2 heads: bf16 10240 bytes, codes 6400, scales 400
     assert call(cache=_cache(vc=KC)) == 6
     assert call(cache=_cache(vc=KC + 6384)) == 6
@@ -132,11 +136,13 @@ def test_rows_error_paths(write):
 
 
 def test_decode4_error_paths():
-    need = apb.decode4_workspace_size(_step())
+    long = _step(capacity=4000, cache_len=3000)
+    need = apb.decode4_workspace_size(long)
+    assert need >= 2 * 8 * 3 * 66 * 4 and apb.decode4_workspace_size(_step()) == 16
 
-    def call(p=None, q=Q, cache=None, o=O, lse=LSE, ws=WS, n=1 << 30, null=False):
+    def call(p=long, q=Q, cache=None, o=O, lse=LSE, ws=WS, n=1 << 30, null=False):
         c = None if null else ctypes.byref(cache or _cache())
-        return apb.lib().apb_decode4_attention(ctypes.byref(p or _step()), q, c, o, lse, 0.0, ws,
+        return apb.lib().apb_decode4_attention(ctypes.byref(p), q, c, o, lse, 0.0, ws,
                                                n, None)
     assert call(null=True) == 1
     assert call(q=None) == 1
@@ -150,8 +156,8 @@ def test_decode4_error_paths():
     assert call(lse=LSE + 2) == 4
     assert call(ws=WS + 8) == 4
     assert call(cache=_cache(kc=KC + 8)) == 4
-    assert call(cache=_cache(vs=VS + 2)) == 4
     assert call(n=need - 1) == 2
+    assert call(_step(), n=15) == 2          # one split needs next to nothing, but not nothing
     assert call(o=Q) == 6
     assert call(o=KC + 16) == 6
     assert call(lse=VS + 396) == 6

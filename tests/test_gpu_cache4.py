@@ -160,6 +160,35 @@ def test_appending_token_by_token_is_one_write():
         assert np.array_equal(whole[n].cpu().numpy(), grown[n].cpu().numpy())
 
 
+def test_on_another_stream_and_in_a_graph():
+    torch = need_gpu()
+    from paper_2502_12085_amd import apb
+    k, v = (dev_bf16(bf16_rows(2, 33, 64, s)) for s in (3, 4))
+    whole = new_cache(2, 40, 64)
+    p = apb.Cache4Problem(2, 64, 40, 7, 33, 33, 0)
+    apb.cache4_write(p, k, v, whole)
+    torch.cuda.synchronize()
+    side, other = torch.cuda.Stream(), new_cache(2, 40, 64)
+    out = [torch.zeros_like(k) for _ in range(4)]
+    torch.cuda.synchronize()
+    apb.cache4_write(p, k, v, other, stream=side)
+    apb.cache4_read(p, other, out[0], out[1], stream=side)
+    side.synchronize()
+    with torch.cuda.stream(side):  # the current stream, which is not the default
+        apb.cache4_read(p, whole, out[2], out[3])
+    side.synchronize()
+    assert all(torch.equal(whole[n], other[n]) for n in whole)
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
+    graph, grown = torch.cuda.CUDAGraph(), new_cache(2, 40, 64)
+    with torch.cuda.graph(graph):
+        apb.cache4_write(p, k, v, grown)
+    for _ in range(3):
+        grown["k_codes"].fill_(FILL)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(whole[n], grown[n]) for n in whole)
+
+
 def test_offsets_past_32_bits():
     # the last head's codes start 4.3 GB into the tensor, its bf16 rows past 2^32 bytes
     torch = need_gpu()

@@ -342,6 +342,89 @@ def test_a_query_that_is_not_a_number():
           keys, d)
 
 
+@pytest.mark.parametrize("rows", [(4, 1, 64, 4), (8, 2, 128, 20)])
+def test_logits_that_overflow(rows):
+    """A key of the largest numbers against queries of 4 and of -4: 64 products of 2^129
+    and more pass fp32's largest number in any order.  NaN for the first, a key without
+    weight for the second, and the other rows as they were."""
+    need_gpu()
+    say(f"[decode4 overflow] {rows}")
+    n_q, n_kv, d, n_new = rows
+    keys = 300
+    q, cache = make(n_q, n_kv, d, keys, keys, n_new, seed=15)
+    q[0, 0], q[n_q - 1, n_new - 1] = 0x4080, 0xC080
+    at = 77
+    cache["k_scales"][:, at] = 252
+    cache["k_codes"][:, at] = 0x77
+    o, lse = run(q, cache, n_kv, keys, keys, 0)
+    assert np.isnan(o[0, 0]).all() and np.isnan(lse[0, 0])
+    k, v = held(cache, keys)
+    k, v = (np.delete(x, at, axis=1) for x in (k, v))
+    ref = oracle.decode4_ref(q, k, v, causal=0, bound=True)
+    last = (slice(n_q - 1, None), slice(n_new - 1, None))
+    check(f"overflow {rows}", (o[last], lse[last]), [x[last] for x in ref], keys, d)
+
+
+@pytest.mark.parametrize("shape", [(8, 2, 64, 401, 400, 2), (8, 2, 128, 700, 699, 9)])
+def test_scales_at_any_address(shape):
+    """Scale bytes from an odd address on, written, read and attended over: bit for bit
+    what they are at an aligned one."""
+    torch = need_gpu()
+    from paper_2502_12085_amd import apb
+    say(f"[decode4 addresses] {shape}")
+    n_q, n_kv, d, cap, keys, n_new = shape
+    q, cache = make(n_q, n_kv, d, cap, keys, n_new, seed=31)
+    want = run(q, cache, n_kv, cap, keys, 1)
+    n = n_kv * cap * (d // 32)
+    moved = dict(cache)
+    for name, at in (("k_scales", 1), ("v_scales", 3)):
+        raw = torch.full((n + 8,), FILL, dtype=torch.uint8, device="cuda")
+        moved[name] = raw[at:at + n].view(n_kv, cap, d // 32)
+        moved[name].copy_(cache[name])
+        assert moved[name].data_ptr() % 4 == at
+    rows = apb.Cache4Problem(n_kv, d, cap, 3, 50, 50, 0)
+    out = [torch.zeros(n_kv, 50, d, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    apb.cache4_read(rows, cache, out[0], out[1])
+    apb.cache4_read(rows, moved, out[2], out[3])
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
+    for name in ("k_scales", "v_scales"):
+        moved[name][:, 3:53] = FILL
+    k, v = (dev_bf16(bf16_rows(n_kv, keys, d, 31 + s, wide=False))[:, 3:53].contiguous()
+            for s in (1, 2))
+    apb.cache4_write(rows, k, v, moved)
+    for name in ("k_scales", "v_scales"):
+        assert torch.equal(moved[name], cache[name])
+    got = run(q, moved, n_kv, cap, keys, 1)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("n_new", [1, 5])
+def test_offsets_past_32_bits(n_new):
+    """2^26 + 5 keys of two heads: the second head's codes start 4.3 GB into the tensor, and
+    so do the last keys' of the first.  Queries of 8 against positive keys in the last
+    300 rows: logits of 50 and more there, so that the others, zeros, weigh less than
+    7e7 e^-50 = 2e-14 together."""
+    torch = need_gpu()
+    from paper_2502_12085_amd import apb
+    say(f"[decode4 long offsets] {n_new} tokens")
+    n_q, n_kv, d, tail = 8, 2, 128, 300
+    keys = (1 << 26) + 5
+    cap = keys + 3
+    cache = new_cache(n_kv, cap, d, fill=0)
+    k = bf16_rows(n_kv, tail, d, 41, wide=False) & 0x7FFF
+    v = bf16_rows(n_kv, tail, d, 42, wide=False)
+    apb.cache4_write(apb.Cache4Problem(n_kv, d, cap, keys - tail, tail, tail, 0), dev_bf16(k),
+                     dev_bf16(v), cache)
+    cache["k_scales"][:, keys:] = 255
+    cache["v_scales"][:, keys:] = 255
+    q = np.full((n_q, n_new, d), 0x4100, np.uint16)
+    q[:, :, ::2] = 0x4110  # 9
+    hk, hv = (oracle.values4_ref(*oracle.quantise4_ref(x)) for x in (k, v))
+    assert (hk.sum(-1) * 8 / d ** 0.5).min() > 50
+    ref = oracle.decode4_ref(q, hk, hv, causal=1, bound=True)
+    check(f"long offsets, {n_new} tokens", run(q, cache, n_kv, cap, keys, 1), ref, tail, d)
+
+
 @pytest.mark.parametrize("shape", [(32, 8, 128, 5000, 4999, 1), (8, 2, 64, 2000, 1999, 90)])
 def test_the_same_every_time_and_on_any_stream(shape):
     torch = need_gpu()
@@ -418,6 +501,34 @@ def test_captured_step(shape):
         torch.cuda.synchronize()
         for a, b in zip(got, (o, lse, k_out, v_out)):
             assert torch.equal(a, b)
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured steps of other shapes over one workspace, replayed in turn: nothing of
+    one is left for the other."""
+    torch = need_gpu()
+    from paper_2502_12085_amd import apb
+    say("[decode4 two graphs]")
+    jobs, ws = [], torch.empty(8 << 20, dtype=torch.uint8, device="cuda")
+    for i, (n_q, n_kv, d, keys, n_new) in enumerate([(32, 8, 128, 6000, 1), (8, 2, 64, 2500, 30)]):
+        q, cache = make(n_q, n_kv, d, keys, keys, n_new, seed=80 + i)
+        want = run(q, cache, n_kv, keys, keys, 1)
+        p = apb.Decode4Problem(n_q, n_kv, d, keys, keys, n_new, 1)
+        assert 16 < apb.decode4_workspace_size(p) <= ws.numel()
+        qd, o = dev_bf16(q), torch.zeros(n_q, n_new, d, device="cuda")
+        lse = torch.zeros(n_q, n_new, device="cuda")
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            apb.decode4_attention(p, qd, cache, o, lse, ws)
+        jobs.append((graph, qd, cache, o, lse, want))
+    for turn in range(3):
+        for graph, _, _, o, lse, want in jobs:
+            o.fill_(turn)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert np.array_equal(o.cpu().numpy(), want[0].astype(np.float32))
+            assert np.array_equal(lse.cpu().numpy(), want[1].astype(np.float32))
 
 
 def test_a_decoding_step_over_three_hosts():

@@ -51,16 +51,16 @@ def _check(problem, plan):
     assert n_split >= 1 and bps >= 1
     assert n_split * bps >= nblk and (n_split - 1) * bps < max(nblk, 1)   # no empty split
     assert n_split == 1 or n_split * row_blocks * n_kv <= 6 * 256         # rounds of the GPU's CUs
-    assert n_split * row_blocks * n_kv < 1 << 31
+    assert n_split * row_blocks * n_kv * 64 * waves < 1 << 32             # threads of a launch
     assert 32 * n_split * bps < (1 << 31) - (1 << 20)                     # key numbers in int32
-    assert ws == n_split * n_q * n_new * (d + 2) * 4
+    assert ws == (n_split * n_q * n_new * (d + 2) * 4 if n_split > 1 else 16)
 
 
 def test_every_key_and_row_once(plans):
     rng = random.Random(5)
     problems = [(1, 1, 64, 0, 1), (8, 2, 64, 0, 3), (1, 1, 128, 1 << 30, 1),
-                (65536, 65536, 128, 1 << 30, 1), (65536, 65536, 64, 33, 16384),
-                (1 << 30, 1, 64, 5, 1), (1, 1, 64, 1 << 30, 1 << 30), (512, 512, 128, 4097, 2),
+                (65536, 65536, 128, 1 << 30, 1), (65536, 65536, 64, 33, 255),
+                ((1 << 24) - 1, 1, 64, 5, 1), (1, 1, 64, 1 << 30, (1 << 24) - 1), (512, 512, 128, 4097, 2),
                 (4096, 64, 64, 100000, 100)]
     for _ in range(3000):
         n_kv = rng.choice((1, 2, 3, 8, 40, 300))
