@@ -395,7 +395,8 @@ apb_status_t apb_decode4_workspace_size(const apb_decode4_problem_t* p, uint64_t
  * and softmax, no rounding of the probabilities, fp32 accumulation and output.  A
  * NaN among a row's visible logits makes its o and lse NaN; a NaN group of a visible
  * V row makes its 32 output elements NaN.  A logit that overflows to -inf is a key
- * without weight, one of +inf or NaN is a NaN.
+ * without weight, one of +inf or NaN is a NaN.  Sums are formed before they are divided:
+ * values of V past 2^76 may overflow.
  */
 apb_status_t apb_decode4_attention(const apb_decode4_problem_t* p, const uint16_t* q,
                                    const apb_cache4_t* cache, float* o_part, float* lse_part,

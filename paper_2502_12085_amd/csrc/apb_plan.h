@@ -193,23 +193,23 @@ inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t
     }
   } else {
     // The splits that make one, two, .. rounds of a workgroup a CU, by what they cost in
-    // blocks of eight waves (1.75 us): a workgroup's own blocks, its start and end (3), and
-    // the partials (1.5 and their bytes).  320 row blocks of 250 key blocks (40 / 8 heads,
-    // 256 tokens) 114 us in one split, 101 so.
+    // blocks of eight waves (1.55 us): a workgroup's own blocks, its start and end (3.5), and
+    // the partials (1.75 and their bytes).  320 row blocks of 250 key blocks (40 / 8 heads,
+    // 256 tokens) 92.5 us in one split, 90.9 so.
     double best = 0;
     for (int64_t r = 1; r <= 6; ++r) {
       const int64_t n = std::max<int64_t>(std::min(kCus * r / base, most), 1);
       const double rounds = (double)((base * n + kCus - 1) / kCus);
       const double partials = (double)n * (double)(n_q * n_new) * (head_dim + 2) * 8;  // there and back
-      const double cost = rounds * ((double)((nblk + 8 * n - 1) / (8 * n)) + 3.0) +
-                          (n > 1 ? 1.5 + partials / 7.9e6 : 0.0);
+      const double cost = rounds * ((double)((nblk + 8 * n - 1) / (8 * n)) + 3.5) +
+                          (n > 1 ? 1.75 + partials / 6.8e6 : 0.0);
       if (r == 1 || cost < best) {
         best = cost;
         n_split = n;
       }
     }
     // one round of eight waves where they have three blocks each (256 rows of 8 heads x
-    // 16448 keys 43.5 -> 40.8 us, x 4000 18.6 -> 18.1; 40 rows x 4000 11.1 against 12.0),
+    // 16448 keys 43.0 -> 37.1 us, x 4000 18.3 -> 18.0; 40 rows x 4000 11.1 against 12.0),
     // else of four, two workgroups a CU where there are as many
     if (base * n_split <= kCus && nblk >= 24 * n_split) pl.waves = 8;
   }

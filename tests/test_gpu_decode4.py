@@ -6,20 +6,21 @@ Bound of an element of o, by its arithmetic.  A logit is an fp32 sum of d produc
 off by at most (d + 8) 2^-24 of sum |q_i k_i| (8: the scale, the base-2 exponent
 and its subtraction of the maximum), doubled for what a matrix instruction's own
 additions may round beside.  A probability carries that as a relative error, and so
-does the sum that divides it: twice; the exponential is good to 2^-22, and a probability
-enters the value product with 2^-17 at least.  The value product and the sum
-add in fp32: blocks of 32 keys one after another in a part, then the parts: (keys / 32 +
-64) 2^-24, doubled as above.  All of it is relative to sum p |v|, which the oracle
-gives.  A probability below 2^-126 of the largest, or what it has below that in
-the sum of its parts, may be flushed to zero: another 2 * 2^-126 max |v| for each key
-(seen with logits that differ by a hundred: an element whose only values are at keys of
-probability 1e-46 is zero in fp32).  The LSE has the logits' error once, its sum's and
-its own rounding.
+does the sum that divides it: twice; the exponential is good to 2^-22.  A probability
+enters the value product as the sum of three bf16 numbers, which hold its 24 bits, or
+of two fp16 ones, each rounded to nearest: the first leaves 2^-12 of it, the second
+2^-12 of that, 2^-24 together where both are normal.  Else the second is off by half the
+2^-24 that fp16 numbers are apart, and the largest probability of a row then stands at
+2^6 at least: 2^-25 / 2^6 = 2^-31 of the largest, which is 1 at most, times max |v| for
+each key.  The value product and the sum add in fp32: blocks of 32 keys one after another
+in a part, then the parts: (keys / 32 + 64) 2^-24, doubled as above.  All of it is
+relative to sum p |v|, which the oracle gives.  The LSE has the logits' error once,
+its sum's and its own rounding.
 
 These are worst cases.  Where logits are of ordinary size the errors of the keys are
-of independent signs, and the norm of o's error is held too: 2^-17 (7.6e-6) of each
-probability, and under 2^-24 sqrt(d) times a logit of 5 (1e-6 to 3e-6) before it, are
-together within 1e-5 of o's norm.
+of independent signs, and the norm of o's error is held too: under 2^-24 sqrt(d) times
+a logit of 5 (1e-6 to 3e-6) of each probability, and 1e-6 of its exponential, parts and
+sum, are together within 1e-5 of o's norm.
 """
 import numpy as np
 import pytest
@@ -38,8 +39,8 @@ V_MAX = 64.0  # no value of these tests' finite rows is larger
 def bounds(keys, d, lse_ref, pv, qk):
     logit = 2 * (d + 8) * 2.0 ** -24 * qk
     add = 2 * (keys / 32 + 64) * 2.0 ** -24
-    o = pv * (2 * logit + 2.0 ** -21 + 2.0 ** -17 + 2 * add)[..., None]
-    o = o + 2 * keys * 2.0 ** -126 * V_MAX
+    o = pv * (2 * logit + 2.0 ** -21 + 2.0 ** -24 + 2 * add)[..., None]
+    o = o + keys * 2.0 ** -31 * V_MAX
     lse = logit + 2.0 ** -22 + add + 2.0 ** -23 * np.abs(np.where(np.isfinite(lse_ref), lse_ref, 0))
     return o, lse
 
@@ -325,6 +326,38 @@ def test_what_a_row_does_not_see(rows):
     cache["k_codes"][:, at] = 0x77
     o, lse = run(q, cache, n_kv, keys, keys, 1)
     check(f"before {rows}", (o[:, ~sees], lse[:, ~sees]), [x[:, ~sees] for x in clean], keys, d)
+
+
+@pytest.mark.parametrize("rows", [(4, 1, 64, 6), (8, 2, 128, 3), (8, 2, 128, 20), (4, 2, 64, 70)])
+def test_values_of_every_size(rows):
+    """Groups of dims whose values are times a power of two, to the ends of what goes into
+    the products as fp16 (scale bytes 108 to 134) and past them: the output is times
+    that power.  Then
+    blocks with a group of zeros under the least scale among the others, in runs and
+    in turn: only the zeros show."""
+    need_gpu()
+    say(f"[decode4 sizes] {rows}")
+    n_q, n_kv, d, n_new = rows
+    keys = 1100
+    groups = d // 32
+    odd = np.repeat(np.random.default_rng(3).integers(0, 2, 35), 32)[:keys].astype(bool)
+    for sizes in ([104, 140, 127, 118], [108, 134, 127, 118], [107, 135, 7, 199],
+                  [108, 20, 134, 190]):
+        q, cache = make(n_q, n_kv, d, keys, keys, n_new, seed=18)
+        cache["v_scales"].fill_(127)
+        k, v = held(cache, keys)
+        scale = np.repeat([2.0 ** (b - 127) for b in sizes[:groups]], 32)
+        for g in range(groups):
+            cache["v_scales"][:, :, g] = sizes[g]
+        o, lse = run(q, cache, n_kv, keys, keys, 1)
+        check(f"sizes {sizes} {rows}", (o / scale, lse),
+              oracle.decode4_ref(q, k, v, causal=1, bound=True), keys, d, norm_bound=1e-5)
+        cache["v_codes"][:, odd, :16] = 0
+        cache["v_scales"][:, odd, 0] = 7
+        v[:, odd, :32] = 0
+        o, lse = run(q, cache, n_kv, keys, keys, 1)
+        check(f"mixed {sizes} {rows}", (o / scale, lse),
+              oracle.decode4_ref(q, k, v, causal=1, bound=True), keys, d, norm_bound=1e-5)
 
 
 def test_a_query_that_is_not_a_number():
