@@ -280,11 +280,15 @@ struct Rows4 {
   }
 
   // The probabilities as P operands, in two fp16 parts or three bf16 ones.
+  // (-1 in a register: the compiler takes a product with it as a difference, in two steps.)
   static __device__ __forceinline__ void parts(const float (&e)[NS], u32x4 (&pr)[PS][2]) {
+    float minus = -1.f;
+    asm("" : "+s"(minus));
 #pragma unroll
     for (int i = 0; i < NS / 2; ++i) {
       const f16x2 hi = to_fp16(e[2 * i], e[2 * i + 1]);
-      const f16x2 lo = to_fp16(fmaf((float)hi[0], -1.f, e[2 * i]), fmaf((float)hi[1], -1.f, e[2 * i + 1]));
+      const f16x2 lo = to_fp16(fmaf((float)hi[0], minus, e[2 * i]),
+                               fmaf((float)hi[1], minus, e[2 * i + 1]));
       pr[i / 4][0][i & 3] = __builtin_bit_cast(unsigned, hi);
       pr[i / 4][1][i & 3] = __builtin_bit_cast(unsigned, lo);
     }
