@@ -193,6 +193,8 @@ def test_long_caches(shape):
     (128, 128, 128, 700, 650, 40, 1),
     (16, 16, 128, 900, 850, 200, 0),
     (14, 7, 64, 500, 450, 100, 0),
+    (7, 1, 128, 1810, 1800, 37, 1),     # 259 rows, 9 to 16 splits
+    (7, 1, 64, 1810, 1800, 37, 0),
 ])
 def test_forms(shape):
     need_gpu()

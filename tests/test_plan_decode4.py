@@ -82,3 +82,12 @@ def test_the_gpu_tests_run_every_form(plans):
     want = {(d, rows, waves, split) for d in (64, 128) for split in (False, True)
             for rows in (16, 32) for waves in (4, 8)}
     assert forms >= want, sorted(want - forms)
+    # and the merge with one, two and all thread groups a row, with a part of a workgroup
+    merges = set()
+    for p, g in zip(problems, plans(problems)):
+        rows = p[0] * p[4]
+        if g[0] > 1:
+            groups = 0 if rows < 256 or g[0] > 16 else 1 if g[0] <= 8 else 2
+            merges.add((p[2], groups, bool(groups) and rows % (1024 // p[2] // groups) != 0))
+    assert merges >= {(d, n, odd) for d in (64, 128) for n in (1, 2) for odd in (True,)}, merges
+    assert merges >= {(64, 0, False), (128, 0, False)}
