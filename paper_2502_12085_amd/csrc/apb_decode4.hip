@@ -450,7 +450,8 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
 
   auto load = [&](const Lane& me, int b) __attribute__((always_inline)) {
     Block x;
-    const int c0 = min(32 * b, p.Lc - 1), last = p.Lc - 1 - c0;  // rows past the last key repeat it
+    // (past the split's last block that again, past the last key that)
+    const int c0 = 32 * min(b, b1 - 1), last = p.Lc - 1 - c0;
     const size_t r0 = (size_t)at.kvh * p.capacity + c0;
     const uint8_t* kc = p.k_codes + r0 * (D / 2);
     const uint8_t* ks = p.k_scales + r0 * G;
@@ -486,8 +487,8 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
   const int row0 = N * at.row_block;
   rows.start(p, at.kvh, row0, [&](int j) { return RUN * Rows::group() + 8 * j; });
 
-  // Block b from x, which takes the wave's next block as soon as it is done with, whatever
-  // b1 (past the last key the loads repeat it).  A second block in flight per wave gained
+  // Block b from x, which takes the wave's next block as soon as it is done with; past the
+  // split's end it asks for its last block, which is on the way anyway.  A second block in flight per wave gained
   // nothing (16385 keys of 8 heads 11.4 against 12.3 us, 524289 110.8 against 112.2): eight
   // waves of a CU have 35 KiB under way.  ODD: V has a group that fp16 does not hold.
   auto block = [&](const Lane& me, Block& x, int b, auto is_odd) __attribute__((always_inline)) {
