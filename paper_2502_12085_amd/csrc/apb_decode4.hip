@@ -20,8 +20,8 @@
 //    place of one, no rounding to speak of.  V is exact in fp16 where its scales are of
 //    ordinary size; blocks with a group that is not, or is NaN, take V in bf16 and the
 //    probabilities in three bf16 parts (the top, middle and lowest 8 bits).  64 tokens
-//    of 32 / 8 heads x 16448 keys 41.4 us all in bf16, 37.6 so; two bf16 parts would
-//    leave 2^-17, and o 2.3e-6 off.
+//    of 32 / 8 heads x 16448 keys 36.9 us with no such block, 42.8 with no other; two
+//    bf16 parts would leave 2^-17, and o 2.3e-6 off.
 //  * Online softmax in base 2 in fp32 with a lazily moved maximum, as in the decode
 //    kernels over bf16: the maximum and O's rescale only when a lane's sum of a block
 //    has grown 2^5 past a block of the maximum.
@@ -488,9 +488,11 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
   rows.start(p, at.kvh, row0, [&](int j) { return RUN * Rows::group() + 8 * j; });
 
   // Block b from x, which takes the wave's next block as soon as it is done with; past the
-  // split's end it asks for its last block, which is on the way anyway.  A second block in flight per wave gained
-  // nothing (16385 keys of 8 heads 11.4 against 12.3 us, 524289 110.8 against 112.2): eight
-  // waves of a CU have 35 KiB under way.  ODD: V has a group that fp16 does not hold.
+  // split's end it asks for its last block, which is on the way anyway (the next split's
+  // would be 26.3 MB of reads in place of 18.1 with one token over 16385 keys of 8 heads).  A
+  // second block in flight per wave gained nothing (those 11.4 against 12.3 us, 524289 keys
+  // 110.8 against 112.2): eight waves of a CU have 35 KiB under way.  ODD: V has a group
+  // that fp16 does not hold.
   auto block = [&](const Lane& me, Block& x, int b, auto is_odd) __attribute__((always_inline)) {
     constexpr bool ODD = decltype(is_odd)::value;
     constexpr int PARTS = ODD ? 3 : 2;
@@ -509,26 +511,29 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
     for (int v = 0; v < VL; ++v) put_group<ODD>(me.put(tile, v), x.vw[v], x.vb[v]);
     if constexpr (ODD) {
       // a group of NaN goes into O by hand, for the rows that see the first key of it
+      bool bad = false;
 #pragma unroll
-      for (int n = 0; n < G; ++n) {
-        int f = 32;
+      for (int v = 0; v < VL; ++v) bad |= x.vb[v] == 255;
+      if (__any(bad)) {
 #pragma unroll
-        for (int v = 0; v < VL; ++v)
-          if (x.vb[v] == 255 && me.g == n) f = min(f, me.v_of[v]);
-        for (int off = 1; off < 64; off *= 2) f = min(f, __shfl_xor(f, off));
-        f = __builtin_amdgcn_readfirstlane(f);
-        if (f < 32) rows.not_a_number(n, c0 + f);
+        for (int n = 0; n < G; ++n) {
+          int f = 32;
+#pragma unroll
+          for (int v = 0; v < VL; ++v)
+            if (x.vb[v] == 255 && me.g == n) f = min(f, me.v_of[v]);
+          for (int off = 1; off < 64; off *= 2) f = min(f, __shfl_xor(f, off));
+          f = __builtin_amdgcn_readfirstlane(f);
+          if (f < 32) rows.not_a_number(n, c0 + f);
+        }
       }
     }
     x = load(me, b + WK);
     // (a wave's LDS accesses are in order; the reads land during the softmax)
     u32x4 v[Rows::NDB][Rows::PS];
-    if constexpr (!ODD) {
 #pragma unroll
-      for (int db = 0; db < Rows::NDB; ++db)
+    for (int db = 0; db < Rows::NDB; ++db)
 #pragma unroll
-        for (int ps = 0; ps < Rows::PS; ++ps) v[db][ps] = Rows::v_operand(v_get, db, ps);
-    }
+      for (int ps = 0; ps < Rows::PS; ++ps) v[db][ps] = Rows::v_operand(v_get, db, ps);
     __builtin_amdgcn_sched_barrier(0);
 
     if (c0 + 32 > vis_all) rows.mask(s, c0);
@@ -541,10 +546,8 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
 #pragma unroll
       for (int t = 0; t < PARTS; ++t)
 #pragma unroll
-        for (int db = 0; db < Rows::NDB; ++db) {
-          if constexpr (ODD) v[db][ps] = Rows::v_operand(v_get, db, ps);
+        for (int db = 0; db < Rows::NDB; ++db)
           rows.template values<ODD>(db, v[db][ps], pr[ps][t]);
-        }
   };
   // Blocks up to the first that is odd, or that is not.  (The asm: each form works out its
   // addresses where its blocks begin, so that the other's keep no registers.)
