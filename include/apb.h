@@ -395,8 +395,9 @@ apb_status_t apb_decode4_workspace_size(const apb_decode4_problem_t* p, uint64_t
  * and softmax, no rounding of the probabilities, fp32 accumulation and output.  A
  * NaN among a row's visible logits makes its o and lse NaN; a NaN group of a visible
  * V row makes its 32 output elements NaN.  A logit that overflows to -inf is a key
- * without weight, one of +inf or NaN is a NaN.  Sums are formed before they are divided:
- * values of V past 2^76 may overflow.
+ * without weight, one of +inf or NaN is a NaN.  Scaled logits past 2^26 in magnitude lie
+ * further apart in fp32 than a softmax tells: such a row may be NaN.  Sums are formed
+ * before they are divided: values of V past 2^76 may overflow.
  */
 apb_status_t apb_decode4_attention(const apb_decode4_problem_t* p, const uint16_t* q,
                                    const apb_cache4_t* cache, float* o_part, float* lse_part,

@@ -400,6 +400,31 @@ def test_logits_that_overflow(rows):
     check(f"overflow {rows}", (o[last], lse[last]), [x[last] for x in ref], keys, d)
 
 
+@pytest.mark.parametrize("rows", [(4, 1, 64, 4, 90), (8, 2, 128, 3, 3000), (8, 2, 128, 20, 900)])
+def test_logits_of_millions(rows):
+    """Logits of 2^22 times N(0, 1): the largest takes all, by far more than an fp32 sum
+    of d products is off, and o is its key's value: a probability over itself, in
+    products and sums of relative error 2^-24 each, a few of them."""
+    need_gpu()
+    say(f"[decode4 millions] {rows}")
+    n_q, n_kv, d, n_new, keys = rows
+    q, cache = make(n_q, n_kv, d, keys, keys, n_new, seed=16)
+    q = (q + (11 << 7)).astype(np.uint16)  # times 2^11
+    cache["k_scales"] += 11
+    k, v = held(cache, keys)
+    s = np.einsum("htd,hkd->htk", oracle.bf16_to_f64(q), np.repeat(k, n_q // n_kv, 0)) / d ** 0.5
+    top = np.sort(s, -1)
+    clear = top[..., -1] - top[..., -2] > 1000
+    assert np.abs(s).max() < 2 ** 26 / 1.4427 and clear.mean() > 0.9
+    o, lse = run(q, cache, n_kv, keys, keys, 0)
+    assert np.isfinite(o).all() and np.isfinite(lse).all()
+    want = np.stack([np.repeat(v, n_q // n_kv, 0)[h][s[h].argmax(-1)] for h in range(n_q)])
+    assert np.all(np.abs(o - want)[clear] <= 2.0 ** -21 * np.abs(want)[clear])
+    # the LSE: a sum of d products and a few roundings of its own
+    qk = np.einsum("htd,hkd->htk", np.abs(oracle.bf16_to_f64(q)), np.abs(np.repeat(k, n_q // n_kv, 0)))
+    assert np.all(np.abs(lse - top[..., -1]) <= 2 * (d + 8) * 2.0 ** -24 * qk.max(-1) / d ** 0.5)
+
+
 @pytest.mark.parametrize("shape", [(8, 2, 64, 401, 400, 2), (8, 2, 128, 700, 699, 9)])
 def test_scales_at_any_address(shape):
     """Scale bytes from an odd address on, written, read and attended over: bit for bit
