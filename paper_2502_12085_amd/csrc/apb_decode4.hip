@@ -7,8 +7,8 @@
 // vector instructions a block to turn codes into operands and to form the softmax.
 // Many rows: the SIMDs' vector instructions, of which a matrix product takes up as
 // much as two (8 cycles of issue whatever its size, 4.7 for an instruction, 8 for a
-// conversion of two codes, 16 for an exponential): 1500 cycles a block of 32 rows, the
-// matrix pipe 800 of them.  So:
+// conversion of two codes, 16 for an exponential): 1800 cycles a block of 32 rows, the
+// matrix pipe 1000 of them.  So:
 //  * A wave owns N = 16 or 32 rows and takes 32-key blocks; the waves of a workgroup
 //    share a split's blocks and meet in LDS at its end, so that a split is one partial.
 //  * S^T = K Q^T on v_mfma_f32_16x16x32_bf16 or v_mfma_f32_32x32x16_bf16 (keys on M,
@@ -16,15 +16,15 @@
 //  * v_cvt_scalef32_pk_bf16_fp4 makes two elements at a time, scale applied: exact.
 //  * O^T = V^T P^T needs 8 keys of one element in a lane: V goes to LDS row by row and
 //    comes back through transposing reads (ds_read_b64_tr_b16).
-//  * The probabilities are two fp16 each, which sum to their 24 bits: two products in
-//    place of one, no rounding to speak of.  V is exact in fp16 where its scales are of
-//    ordinary size; blocks with a group that is not, or is NaN, take V in bf16 and the
-//    probabilities in three bf16 parts (the top, middle and lowest 8 bits).  64 tokens
-//    of 32 / 8 heads x 16448 keys 36.9 us with no such block, 42.8 with no other; two
-//    bf16 parts would leave 2^-17, and o 2.3e-6 off.
+//  * The probabilities are three bf16 each, the top, middle and lowest 8 bits of
+//    their fp32 significand: three products in place of one, no rounding, whatever their
+//    size beside the row's largest.  Two bf16 parts leave 2^-17, and o 2.3e-6 off.  Two
+//    fp16 parts cost half the instructions (64 tokens of 32 / 8 heads x 16448 keys 35.6 us
+//    against 40.5) but end at 2^-24: behind a key 14 nats above the others, with values
+//    of zero, o is 1e-4 off, at 22 nats gone.
 //  * Online softmax in base 2 in fp32 with a lazily moved maximum, as in the decode
 //    kernels over bf16: the maximum and O's rescale only when a lane's sum of a block
-//    has grown 2^5 past a block of the maximum.
+//    passes 2^13.
 #include <math.h>
 
 #include <type_traits>
@@ -36,8 +36,6 @@ namespace apb {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -46,11 +44,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 
-// A probability is 2^kShift at the maximum when that moves, and a lane's sum of a block may
-// grow to kSumLimit before it moves again, half of fp16's largest number.  The two fp16 parts
-// hold a probability to 2^-24 of itself, or to the 2^-25 that fp16 ends at, 2^-31 of the
-// largest.
-constexpr float kShift = 6.f, kSumLimit = 32768.f;
+constexpr float kSumLimit = 8192.f;  // largest lane sum of a block against a stale maximum
 
 struct Dec4Params {
   const uint16_t* q;
@@ -77,30 +71,6 @@ __device__ __forceinline__ u32x4 elements(unsigned w, float scale) {
   return x;
 }
 
-__device__ __forceinline__ u32x4 elements16(unsigned w, float scale) {  // as fp16
-  u32x4 x;
-  x[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0));
-  x[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1));
-  x[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2));
-  x[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3));
-  return x;
-}
-
-// Both to the nearest fp16 numbers.  (The empty asm keeps the pair together: the compiler
-// would convert the first of a split one by one as well.)
-__device__ __forceinline__ f16x2 to_fp16(float a, float b) {
-  const f16x2 y = {(_Float16)a, (_Float16)b};
-  unsigned bits = __builtin_bit_cast(unsigned, y);
-  asm("" : "+v"(bits));
-  return __builtin_bit_cast(f16x2, bits);
-}
-
-// V goes into the products times 2^kVShift, by which fp16 holds every value of a group with
-// scale byte 114 - kVShift .. 140 - kVShift as a normal number (largest magnitudes of 7e-6
-// to 900): a sum of products with subnormal operands loses as many bits as they lack.
-constexpr int kVShift = 6;
-__device__ __forceinline__ bool fits_fp16(unsigned b) { return b - (114u - kVShift) <= 26u; }
-
 __device__ __forceinline__ bf16x8 as_bf16(u32x4 x) { return __builtin_bit_cast(bf16x8, x); }
 
 __device__ __forceinline__ f32x4 product(const bf16x8& a, const bf16x8& b, const f32x4& c) {
@@ -110,14 +80,7 @@ __device__ __forceinline__ f32x16 product(const bf16x8& a, const bf16x8& b, cons
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-__device__ __forceinline__ f32x4 product(const f16x8& a, const f16x8& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x16 product(const f16x8& a, const f16x8& b, const f32x16& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-}
-
-// A V tile of 32 keys in LDS, 16 bits an element row by row, chunk (16 bytes) c of key r at chunk c ^ swz(r).
+// A V tile of 32 keys in LDS, bf16 row by row, chunk (16 bytes) c of key r at chunk c ^ swz(r).
 // A clock serves 16 lanes' 16 bytes or 32 lanes' transposing reads, on 64 banks (256 bytes,
 // one row of d = 128, two of 64).
 // Transposing reads take 8 keys x 32 bytes (N = 16) or 4 keys x 64 bytes (N = 32).
@@ -138,18 +101,11 @@ __device__ __forceinline__ int v_key(int x) {
                  : hi | (x & 1) | (x & 6) << 1 | (x & 8) >> 2;      // r0, r2, r3, then r1
 }
 
-// A group's 32 elements into its row's four chunks at `at` (exclusive or 16 j), as fp16 or
-// (ODD) as bf16.  A group of NaN goes there as zeros: in a product a zero probability
-// would not keep it out.
-template <bool ODD>
+// A group's 32 elements into its row's four chunks at `at` (exclusive or 16 j).
 __device__ __forceinline__ void put_group(uint32_t at, const u32x4& codes, unsigned b) {
-  const bool bad = ODD && b == 255;
-  const float scale = __uint_as_float(bad ? 0u : (ODD ? b : b + kVShift) << 23);
+  const float scale = __uint_as_float(b << 23);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const unsigned w = codes[j];
-    *(lds_u32x4*)(uintptr_t)(at ^ (16u * j)) = ODD ? elements(bad ? 0u : w, scale) : elements16(w, scale);
-  }
+  for (int j = 0; j < 4; ++j) *(lds_u32x4*)(uintptr_t)(at ^ (16u * j)) = elements(codes[j], scale);
 }
 
 __device__ __forceinline__ uint32_t lds_base(const void* p) {
@@ -257,7 +213,7 @@ struct Rows4 {
       for (int i = 1; i < NS; ++i) mx = fmaxf(mx, logit(s, i));
 #pragma unroll
       for (int off = N; off < 64; off *= 2) mx = fmaxf(mx, __shfl_xor(mx, off));
-      const float m_new = fmaxf(m_run, mx * scale - kShift);
+      const float m_new = fmaxf(m_run, mx * scale);
       if (m_new == -INFINITY) {
         // nothing but keys that the row does not see, and NaN, which stays
         sum = 0.f;
@@ -279,29 +235,15 @@ struct Rows4 {
     l_run += sum;
   }
 
-  // The probabilities as P operands, in two fp16 parts or three bf16 ones.
-  // (-1 in a register: the compiler takes a product with it as a difference, in two steps.)
-  static __device__ __forceinline__ void parts(const float (&e)[NS], u32x4 (&pr)[PS][2]) {
-    float minus = -1.f;
-    asm("" : "+s"(minus));
-#pragma unroll
-    for (int i = 0; i < NS / 2; ++i) {
-      const f16x2 hi = to_fp16(e[2 * i], e[2 * i + 1]);
-      const f16x2 lo = to_fp16(fmaf((float)hi[0], minus, e[2 * i]),
-                               fmaf((float)hi[1], minus, e[2 * i + 1]));
-      pr[i / 4][0][i & 3] = __builtin_bit_cast(unsigned, hi);
-      pr[i / 4][1][i & 3] = __builtin_bit_cast(unsigned, lo);
-    }
-  }
+  // The probabilities as P operands, in their three parts.
   static __device__ __forceinline__ void parts(const float (&e)[NS], u32x4 (&pr)[PS][3]) {
 #pragma unroll
     for (int i = 0; i < NS / 2; ++i) {
       unsigned hi[2], mid[2], lo[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const float x = e[2 * i + t] * (float)(1 << kVShift);  // (in place of V, that has no room)
-        hi[t] = __float_as_uint(x);
-        const float r1 = x - __uint_as_float(hi[t] & 0xFFFF0000u);
+        hi[t] = __float_as_uint(e[2 * i + t]);
+        const float r1 = e[2 * i + t] - __uint_as_float(hi[t] & 0xFFFF0000u);
         mid[t] = __float_as_uint(r1);
         lo[t] = __float_as_uint(r1 - __uint_as_float(mid[t] & 0xFFFF0000u));
       }
@@ -321,7 +263,7 @@ struct Rows4 {
     return tile + (uint32_t)(key * 2 * D + 16 * (chunk ^ v_swz<D, N>(key)) + 8 * (sl & 1));
   }
   // The V operand of dim block db and P operand ps: two of them, 8 or 16 keys apart.
-  static __device__ __forceinline__ u32x4 v_operand(uint32_t v_get, int db, int ps) {
+  static __device__ __forceinline__ bf16x8 v_operand(uint32_t v_get, int db, int ps) {
     i16x4 part[2];
 #pragma unroll
     for (int rd = 0; rd < 2; ++rd) {
@@ -330,14 +272,12 @@ struct Rows4 {
       part[rd] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (lds_i16x4*)(uintptr_t)(a + (uint32_t)((16 * ps + (kWide ? 8 : 16) * rd) * 2 * D)));
     }
-    return __builtin_bit_cast(u32x4,
+    return __builtin_bit_cast(bf16x8,
                               __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
   }
-  // O^T += V^T P^T: one part of one P operand, one dim block, of fp16 or (ODD) of bf16.
-  template <bool ODD>
-  __device__ __forceinline__ void values(int db, const u32x4& v, const u32x4& p) {
-    if constexpr (ODD) oacc[db] = product(as_bf16(v), as_bf16(p), oacc[db]);
-    else oacc[db] = product(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, p), oacc[db]);
+  // O^T += V^T P^T: one part of one P operand, one dim block.
+  __device__ __forceinline__ void values(int db, const bf16x8& v, const u32x4& p) {
+    oacc[db] = product(v, as_bf16(p), oacc[db]);
   }
 
   // Values of group g (dims 32 g ..) of key c are NaN: so is O of the row if it sees it.
@@ -391,7 +331,6 @@ struct Rows4 {
         l = fmaf(w, lk, l);
         y += w * *reinterpret_cast<const f32x4*>(o_lds + k * OUT + r * (4 * D) + 16 * (c ^ (r & 15)));
       }
-      y *= 1.f / (1 << kVShift);
       const size_t row = (size_t)at.kvh * p.R + row0 + r;
       if constexpr (WHOLE) {
         *reinterpret_cast<f32x4*>(p.o + row * D + 4 * c) = y * (l == 0.f ? 0.f : 1.f / l);
@@ -431,16 +370,15 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
 
   // Where a lane works in a block: of K it takes its part of each tile's key, of V whole
   // groups, of keys v_of.
-  struct Lane {
-    int lr, lg, g, v_of[VL];
-    __device__ __forceinline__ explicit Lane(int lane) : lr(lane % N), lg(lane / N), g(lane % G) {
+  const int lane = threadIdx.x & 63, lr = Rows::lane_row(), lg = Rows::group(), g = lane % G;
+  int v_of[VL];
+  uint32_t v_put[VL];
 #pragma unroll
-      for (int v = 0; v < VL; ++v) v_of[v] = v_key<D, N>((64 * v + lane) / G);
-    }
-    __device__ __forceinline__ uint32_t put(uint32_t tile, int v) const {
-      return tile + (uint32_t)(v_of[v] * 2 * D + 16 * ((4 * g) ^ v_swz<D, N>(v_of[v])));
-    }
-  };
+  for (int v = 0; v < VL; ++v) {
+    v_of[v] = v_key<D, N>((64 * v + lane) / G);
+    v_put[v] = tile + (uint32_t)(v_of[v] * 2 * D + 16 * ((4 * g) ^ v_swz<D, N>(v_of[v])));
+  }
+  const uint32_t v_get = Rows::v_lane(tile);
   // The codes and scale bytes that a lane takes of a block.
   struct Block {
     unsigned kw[Rows::TILES][KW], kb[Rows::TILES][KB];
@@ -448,7 +386,7 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
     unsigned vb[VL];
   };
 
-  auto load = [&](const Lane& me, int b) __attribute__((always_inline)) {
+  auto load = [&](int b) __attribute__((always_inline)) {
     Block x;
     // (past the split's last block that again, past the last key that)
     const int c0 = 32 * min(b, b1 - 1), last = p.Lc - 1 - c0;
@@ -459,45 +397,41 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
     const uint8_t* vs = p.v_scales + r0 * G;
 #pragma unroll
     for (int i = 0; i < Rows::TILES; ++i) {
-      const uint32_t key = (uint32_t)min(N * i + me.lr, last);
+      const uint32_t key = (uint32_t)min(N * i + lr, last);
       if constexpr (RUN >= 32) {
 #pragma unroll
         for (int h = 0; h < KB; ++h) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(kc + (key * (D / 2) + (RUN / 2) * me.lg + 16u * h));
+          const u32x4 w = *reinterpret_cast<const u32x4*>(kc + (key * (D / 2) + (RUN / 2) * lg + 16u * h));
           x.kw[i][4 * h] = w[0]; x.kw[i][4 * h + 1] = w[1];
           x.kw[i][4 * h + 2] = w[2]; x.kw[i][4 * h + 3] = w[3];
-          x.kb[i][h] = ks[key * G + KB * me.lg + h];
+          x.kb[i][h] = ks[key * G + KB * lg + h];
         }
       } else {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(kc + (key * (D / 2) + (RUN / 2) * me.lg));
+        const u32x2 w = *reinterpret_cast<const u32x2*>(kc + (key * (D / 2) + (RUN / 2) * lg));
         x.kw[i][0] = w[0]; x.kw[i][1] = w[1];
-        x.kb[i][0] = ks[key * G + RUN * me.lg / 32];
+        x.kb[i][0] = ks[key * G + RUN * lg / 32];
       }
     }
 #pragma unroll
     for (int v = 0; v < VL; ++v) {
-      const uint32_t key = (uint32_t)min(me.v_of[v], last);
-      x.vw[v] = *reinterpret_cast<const u32x4*>(vc + (key * (D / 2) + 16u * me.g));
-      x.vb[v] = vs[key * G + me.g];
+      const uint32_t key = (uint32_t)min(v_of[v], last);
+      x.vw[v] = *reinterpret_cast<const u32x4*>(vc + (key * (D / 2) + 16u * g));
+      x.vb[v] = vs[key * G + g];
     }
     return x;
   };
 
   Rows rows;
   const int row0 = N * at.row_block;
-  rows.start(p, at.kvh, row0, [&](int j) { return RUN * Rows::group() + 8 * j; });
+  rows.start(p, at.kvh, row0, [&](int j) { return RUN * lg + 8 * j; });
 
   // Block b from x, which takes the wave's next block as soon as it is done with; past the
   // split's end it asks for its last block, which is on the way anyway (the next split's
   // would be 26.3 MB of reads in place of 18.1 with one token over 16385 keys of 8 heads).  A
   // second block in flight per wave gained nothing (those 11.4 against 12.3 us, 524289 keys
-  // 110.8 against 112.2): eight waves of a CU have 35 KiB under way.  ODD: V has a group
-  // that fp16 does not hold.
-  auto block = [&](const Lane& me, Block& x, int b, auto is_odd) __attribute__((always_inline)) {
-    constexpr bool ODD = decltype(is_odd)::value;
-    constexpr int PARTS = ODD ? 3 : 2;
+  // 110.8 against 112.2): eight waves of a CU have 35 KiB under way.
+  auto block = [&](Block& x, int b) __attribute__((always_inline)) {
     const int c0 = 32 * b;
-    const uint32_t v_get = Rows::v_lane(tile);
     typename Rows::Acc s[Rows::TILES];
 #pragma unroll
     for (int i = 0; i < Rows::TILES; ++i)
@@ -507,29 +441,34 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
         rows.logits(s[i], as_bf16(elements(x.kw[i][j], scale)), j);
       }
 
+    // A group of NaN goes into O by hand, for the rows that see the first key of it, and
+    // into the tile as zeros: in a product a zero probability would not keep it out.
+    bool bad = false;
 #pragma unroll
-    for (int v = 0; v < VL; ++v) put_group<ODD>(me.put(tile, v), x.vw[v], x.vb[v]);
-    if constexpr (ODD) {
-      // a group of NaN goes into O by hand, for the rows that see the first key of it
-      bool bad = false;
+    for (int v = 0; v < VL; ++v) bad |= x.vb[v] == 255;
+    if (__any(bad)) {
 #pragma unroll
-      for (int v = 0; v < VL; ++v) bad |= x.vb[v] == 255;
-      if (__any(bad)) {
+      for (int n = 0; n < G; ++n) {
+        int f = 32;
 #pragma unroll
-        for (int n = 0; n < G; ++n) {
-          int f = 32;
-#pragma unroll
-          for (int v = 0; v < VL; ++v)
-            if (x.vb[v] == 255 && me.g == n) f = min(f, me.v_of[v]);
-          for (int off = 1; off < 64; off *= 2) f = min(f, __shfl_xor(f, off));
-          f = __builtin_amdgcn_readfirstlane(f);
-          if (f < 32) rows.not_a_number(n, c0 + f);
-        }
+        for (int v = 0; v < VL; ++v)
+          if (x.vb[v] == 255 && g == n) f = min(f, v_of[v]);
+        for (int off = 1; off < 64; off *= 2) f = min(f, __shfl_xor(f, off));
+        f = __builtin_amdgcn_readfirstlane(f);
+        if (f < 32) rows.not_a_number(n, c0 + f);
       }
+#pragma unroll
+      for (int v = 0; v < VL; ++v)
+        if (x.vb[v] == 255) {
+          x.vw[v] = u32x4{};
+          x.vb[v] = 127;
+        }
     }
-    x = load(me, b + WK);
+#pragma unroll
+    for (int v = 0; v < VL; ++v) put_group(v_put[v], x.vw[v], x.vb[v]);
+    x = load(b + WK);
     // (a wave's LDS accesses are in order; the reads land during the softmax)
-    u32x4 v[Rows::NDB][Rows::PS];
+    bf16x8 v[Rows::NDB][Rows::PS];
 #pragma unroll
     for (int db = 0; db < Rows::NDB; ++db)
 #pragma unroll
@@ -539,38 +478,18 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
     if (c0 + 32 > vis_all) rows.mask(s, c0);
     float e[Rows::NS];
     rows.softmax(s, p.scale_log2, e);
-    u32x4 pr[Rows::PS][PARTS];
+    u32x4 pr[Rows::PS][3];
     Rows::parts(e, pr);
 #pragma unroll
     for (int ps = 0; ps < Rows::PS; ++ps)
 #pragma unroll
-      for (int t = 0; t < PARTS; ++t)
+      for (int t = 0; t < 3; ++t)
 #pragma unroll
-        for (int db = 0; db < Rows::NDB; ++db)
-          rows.template values<ODD>(db, v[db][ps], pr[ps][t]);
+        for (int db = 0; db < Rows::NDB; ++db) rows.values(db, v[db][ps], pr[ps][t]);
   };
-  // Blocks up to the first that is odd, or that is not.  (The asm: each form works out its
-  // addresses where its blocks begin, so that the other's keep no registers.)
-  auto blocks = [&](Block& x, int& b, auto is_odd) __attribute__((always_inline)) {
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));
-    const Lane me(lane);
-#pragma unroll 1
-    for (; b < b1; b += WK) {
-      bool fits = true;
-#pragma unroll
-      for (int v = 0; v < VL; ++v) fits &= fits_fp16(x.vb[v]);
-      if ((bool)__all(fits) == decltype(is_odd)::value) break;
-      block(me, x, b, is_odd);
-    }
-  };
-  int b = b0 + wave;
-  if (b < b1) {
-    Block x = load(Lane(threadIdx.x & 63), b);
-    do {
-      blocks(x, b, std::false_type{});
-      blocks(x, b, std::true_type{});
-    } while (b < b1);
+  if (b0 + wave < b1) {
+    Block x = load(b0 + wave);
+    for (int b = b0 + wave; b < b1; b += WK) block(x, b);
   }
   rows.template finish<WK, WHOLE>(p, at, row0, wave, lds, ml_lds);
 }

@@ -1,0 +1,144 @@
+"""Decoding attention over a KV cache in 4 bits where probabilities of every size count:
+one key far above the rest whose values are zero (an attention sink), so that o is made
+of probabilities that are tiny beside the largest.
+
+Bound of an element of o: that of ``test_gpu_decode4``, relative to sum p |v|, without its
+absolute term.  A probability enters the value product with its 24 bits whatever its size,
+down to where fp32 itself ends: 2^-126 of the largest, times max |v|, for each key, twice
+over.
+
+Norm of o's error, shapes of N(0, 1): a logit of a few units is a sum of d terms whose
+partial sums are rounded to 2^-24 of themselves, 2e-7 of a probability at d = 128; its
+base-2 exponent, 8 to 16 in magnitude, is rounded to half of 2^-20, 3.3e-7; the
+exponential, the parts and the sums are 2e-7 together.  Of independent signs over the keys
+they are below 1e-6 of o's norm.  Behind a sink of g nats the exponent is up to 128 in
+magnitude, rounded to half of 2^-17 (2.6e-6 of a probability): 1e-5.
+"""
+import numpy as np
+import pytest
+
+import oracle
+import test_gpu_decode4 as base
+from paper_2502_12085_amd import inputs
+from gpu_util import dev_bf16, need_gpu, say
+from test_gpu_cache4 import bf16_rows, new_cache
+
+pytestmark = pytest.mark.gpu
+
+ORDINARY = list(dict.fromkeys(
+    s for f in (base.test_matches_oracle, base.test_forms) for m in f.pytestmark
+    if m.name == "parametrize" for s in m.args[1]))
+
+# every form of the kernel: head size, 16 or 32 rows a wave, four or eight waves, one split
+# or several (a CPU test holds that)
+SINKS = [
+    # n_q, n_kv, d, capacity, cache_len, n_new, causal
+    (4, 1, 64, 130, 128, 4, 1),
+    (4, 1, 64, 1021, 515, 3, 1),
+    (8, 2, 128, 120, 100, 3, 1),
+    (8, 2, 128, 500, 400, 3, 0),
+    (4, 1, 64, 100, 97, 7, 1),
+    (8, 1, 128, 100, 90, 6, 1),
+    (4, 1, 64, 300, 300, 5, 1),
+    (8, 1, 128, 300, 290, 4, 0),
+    (8, 2, 64, 2100, 2000, 1, 1),
+    (8, 8, 128, 1000, 1000, 1, 1),
+    (32, 8, 128, 4500, 4097, 1, 1),
+    (8, 2, 64, 30000, 29000, 1, 1),
+    (32, 8, 128, 16390, 16385, 1, 1),
+    (4, 1, 64, 2000, 1999, 7, 1),
+    (8, 1, 128, 2000, 1777, 4, 0),
+    (8, 1, 64, 50000, 49000, 5, 1),
+    (8, 1, 128, 50000, 49000, 5, 0),
+    (32, 8, 128, 2200, 2112, 64, 1),
+    (120, 120, 64, 1700, 1650, 17, 1),
+    (120, 120, 128, 1700, 1650, 17, 0),
+    (300, 300, 64, 200, 199, 1, 1),
+    (260, 260, 64, 140, 131, 70, 1),
+]
+
+
+def check(what, got, ref, keys, d, norm_bound):
+    (o, lse), (ro, rl, pv, qk) = got, ref
+    _, bl = base.bounds(keys, d, rl, pv, qk)
+    logit, add = 2 * (d + 8) * 2.0 ** -24 * qk, 2 * (keys / 32 + 64) * 2.0 ** -24
+    bo = pv * (2 * logit + 2.0 ** -21 + 2.0 ** -24 + 2 * add)[..., None]
+    bo = bo + 2 * keys * 2.0 ** -126 * base.V_MAX
+    assert np.isfinite(o).all() and np.isfinite(lse).all(), what
+    eo, el = np.abs(o - ro), np.abs(lse - rl)
+    norm = np.linalg.norm(o - ro) / np.linalg.norm(ro)
+    say(f"  {what}: o {norm:.2e} of its norm, worst {(eo / bo).max():.3f} of its bound, lse "
+        f"{(el / bl).max():.3f} of its")
+    assert norm <= norm_bound, what
+    assert np.all(eo <= bo) and np.all(el <= bl), what
+
+
+@pytest.mark.parametrize("shape", ORDINARY)
+def test_ordinary_logits(shape):
+    need_gpu()
+    say(f"[decode4 range] {shape}")
+    n_q, n_kv, d, cap, keys, n_new, causal = shape
+    q, cache = base.make(n_q, n_kv, d, cap, keys, n_new, seed=keys + 1)
+    k, v = base.held(cache, keys)
+    got = base.run(q, cache, n_kv, cap, keys, causal)
+    check(f"ordinary {shape}", got, oracle.decode4_ref(q, k, v, causal=causal, bound=True), keys,
+          d, 1e-6)
+
+
+@pytest.mark.parametrize("every", [0, 97])
+@pytest.mark.parametrize("shape", SINKS)
+def test_sinks(shape, every):
+    """Key 0 (and with ``every`` each 97th) g nats above the others, its values zero: 32
+    elements of q are equal, and those of the others' K zero."""
+    torch = need_gpu()
+    from paper_2502_12085_amd import apb
+    say(f"[decode4 sinks] {shape} {every}")
+    n_q, n_kv, d, cap, keys, n_new, causal = shape
+    q = inputs.bf16_bits_to_f32(bf16_rows(n_q, n_new, d, 1, wide=False)).copy()
+    k, v = (inputs.bf16_bits_to_f32(bf16_rows(n_kv, keys, d, s, wide=False)).copy()
+            for s in (2, 3))
+    at = slice(0, keys, every) if every else slice(0, 1)
+    k[:, :, :32] = 0
+    k[:, at] = 0
+    k[:, at, :32] = 4
+    v[:, at] = 0
+    cache = new_cache(n_kv, cap, d, fill=0xFF)
+    apb.cache4_write(apb.Cache4Problem(n_kv, d, cap, 0, keys, keys, 0),
+                     *(dev_bf16(inputs.f32_to_bf16_bits(x)) for x in (k, v)), cache)
+    cache["v_scales"][:, at] = 127  # zeros of an ordinary scale
+    torch.cuda.synchronize()
+    hk, hv = base.held(cache, keys)
+    for g in (10, 14, 18, 22, 50):
+        q[:, :, :32] = g * d ** 0.5 / (32 * 4)
+        bits = inputs.f32_to_bf16_bits(q)
+        ref = oracle.decode4_ref(bits, hk, hv, causal=causal, bound=True)
+        got = base.run(bits, cache, n_kv, cap, keys, causal)
+        check(f"{g} nats {shape} {every}", got, ref, keys, d, 1e-5)
+
+
+@pytest.mark.parametrize("rows", base.ROWS)
+def test_values_of_one_group_behind_a_sink(rows):
+    """The sink's values are zero in the first 32 elements and large in the others: the
+    small probabilities count in the first alone."""
+    torch = need_gpu()
+    from paper_2502_12085_amd import apb
+    say(f"[decode4 group behind a sink] {rows}")
+    n_q, n_kv, d, n_new = rows
+    keys = 1300
+    q = inputs.bf16_bits_to_f32(bf16_rows(n_q, n_new, d, 1, wide=False)).copy()
+    k, v = (inputs.bf16_bits_to_f32(bf16_rows(n_kv, keys, d, s, wide=False)).copy()
+            for s in (2, 3))
+    k[:, :, :32], k[:, 0], k[:, 0, :32] = 0, 0, 4
+    v[:, 0], v[:, 0, 32:] = 0, 6
+    q[:, :, :32] = 20 * d ** 0.5 / (32 * 4)
+    cache = new_cache(n_kv, keys, d, fill=0xFF)
+    apb.cache4_write(apb.Cache4Problem(n_kv, d, keys, 0, keys, keys, 0),
+                     *(dev_bf16(inputs.f32_to_bf16_bits(x)) for x in (k, v)), cache)
+    cache["v_scales"][:, 0, 0] = 127
+    torch.cuda.synchronize()
+    bits = inputs.f32_to_bf16_bits(q)
+    ref = oracle.decode4_ref(bits, *base.held(cache, keys), causal=1, bound=True)
+    o, lse = base.run(bits, cache, n_kv, keys, keys, 1)
+    for dims in (slice(0, 32), slice(32, None)):
+        check(f"group {rows} {dims}", (o[..., dims], lse),
+              (ref[0][..., dims], ref[1], ref[2][..., dims], ref[3]), keys, d, 1e-5)
