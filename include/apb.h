@@ -395,7 +395,7 @@ apb_status_t apb_decode4_workspace_size(const apb_decode4_problem_t* p, uint64_t
  * and softmax, no rounding of the probabilities (however small they are beside the
  * row's largest, down to 2^-126 of it), fp32 accumulation and output.  A NaN among a
  * row's visible logits makes its o and lse NaN; a NaN group of a visible V row makes its
- * 32 output elements NaN.  A logit that overflows to -inf is a key
+ * 32 output elements NaN, and so does one under a scale byte of 253 or 254.  A logit that overflows to -inf is a key
  * without weight, one of +inf or NaN is a NaN.  Scaled logits past 2^26 in magnitude lie
  * further apart in fp32 than a softmax tells: such a row may be NaN.  Sums are formed
  * before they are divided: values of V past 2^76 may overflow.

@@ -101,6 +101,9 @@ __device__ __forceinline__ int v_key(int x) {
                  : hi | (x & 1) | (x & 6) << 1 | (x & 8) >> 2;      // r0, r2, r3, then r1
 }
 
+// Scale bytes whose groups the products do not take: of 253 on 6 * 2^(b - 127) is infinite.
+__device__ __forceinline__ bool not_finite(unsigned b) { return b > 252; }
+
 // A group's 32 elements into its row's four chunks at `at` (exclusive or 16 j).
 __device__ __forceinline__ void put_group(uint32_t at, const u32x4& codes, unsigned b) {
   const float scale = __uint_as_float(b << 23);
@@ -441,25 +444,26 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
         rows.logits(s[i], as_bf16(elements(x.kw[i][j], scale)), j);
       }
 
-    // A group of NaN goes into O by hand, for the rows that see the first key of it, and
-    // into the tile as zeros: in a product a zero probability would not keep it out.
+    // A group that is not finite (NaN, or under a scale past bf16's numbers) goes into O by
+    // hand, for the rows that see the first key of it, and into the tile as zeros: in a
+    // product a zero probability would not keep it out.
     bool bad = false;
 #pragma unroll
-    for (int v = 0; v < VL; ++v) bad |= x.vb[v] == 255;
+    for (int v = 0; v < VL; ++v) bad |= not_finite(x.vb[v]);
     if (__any(bad)) {
 #pragma unroll
       for (int n = 0; n < G; ++n) {
         int f = 32;
 #pragma unroll
         for (int v = 0; v < VL; ++v)
-          if (x.vb[v] == 255 && g == n) f = min(f, v_of[v]);
+          if (not_finite(x.vb[v]) && g == n) f = min(f, v_of[v]);
         for (int off = 1; off < 64; off *= 2) f = min(f, __shfl_xor(f, off));
         f = __builtin_amdgcn_readfirstlane(f);
         if (f < 32) rows.not_a_number(n, c0 + f);
       }
 #pragma unroll
       for (int v = 0; v < VL; ++v)
-        if (x.vb[v] == 255) {
+        if (not_finite(x.vb[v])) {
           x.vw[v] = u32x4{};
           x.vb[v] = 127;
         }

@@ -142,3 +142,35 @@ def test_values_of_one_group_behind_a_sink(rows):
     for dims in (slice(0, 32), slice(32, None)):
         check(f"group {rows} {dims}", (o[..., dims], lse),
               (ref[0][..., dims], ref[1], ref[2][..., dims], ref[3]), keys, d, 1e-5)
+
+
+@pytest.mark.parametrize("rows", [(4, 1, 64, 6), (8, 2, 128, 3), (8, 2, 128, 20), (4, 2, 64, 70)])
+def test_unseen_rows_of_any_bytes(rows):
+    """Every scale byte and the largest codes in a row among the new tokens' own, of K, of V
+    and of both: the tokens before it are as if it were not there.  Scale bytes past 252 in V
+    are past bf16's largest number: NaN in their 32 elements, for those that see them."""
+    need_gpu()
+    say(f"[decode4 any bytes] {rows}")
+    n_q, n_kv, d, n_new = rows
+    keys = 200 + n_new
+    q, cache = base.make(n_q, n_kv, d, keys, keys, n_new, seed=5)
+    k, v = base.held(cache, keys)
+    clean = oracle.decode4_ref(q, k, v, causal=1, bound=True)
+    at = keys - n_new // 2  # tokens j >= n_new - n_new // 2 see it
+    sees = np.arange(n_new) >= n_new - n_new // 2
+    kept = {n: t.clone() for n, t in cache.items()}
+    for which in ("v", "k", "kv"):
+        for b in (0, 1, 6, 7, 127, 251, 252, 253, 254, 255):
+            for n in which:
+                cache[n + "_scales"][:, at] = kept[n + "_scales"][:, at]
+                cache[n + "_scales"][:, at, 1] = b
+                cache[n + "_codes"][:, at] = 0xF7  # 6 and -6
+            o, lse = base.run(q, cache, n_kv, keys, keys, 1)
+            check(f"{which} {b} {rows}", (o[:, ~sees], lse[:, ~sees]),
+                  [x[:, ~sees] for x in clean], keys, d, 1e-6)
+            if which == "v":
+                bad = np.isnan(o[:, sees])
+                assert bad[..., 32:64].all() if b > 252 else not bad.any()
+                assert not bad[..., :32].any() and not bad[..., 64:].any()
+        for n, t in kept.items():
+            cache[n].copy_(t)
