@@ -174,3 +174,28 @@ def test_unseen_rows_of_any_bytes(rows):
                 assert not bad[..., :32].any() and not bad[..., 64:].any()
         for n, t in kept.items():
             cache[n].copy_(t)
+
+
+@pytest.mark.parametrize("shape", [(4, 1, 64, 140, 1, 32), (8, 2, 64, 2000, 1, 128),
+                                   (8, 2, 128, 2000, 9, 128), (14, 7, 64, 450, 100, 128),
+                                   (7, 1, 128, 1800, 37, 128)])
+def test_nan_among_keys_without_weight(shape):
+    """The first keys overflow to logits of -inf for every row, 64 products of -2^129 and
+    more: they have no weight, a whole split of them either, but a NaN group of their
+    values is one of visible rows, and its 32 elements of o are NaN."""
+    need_gpu()
+    say(f"[decode4 no weight] {shape}")
+    n_q, n_kv, d, keys, n_new, n = shape
+    q, cache = base.make(n_q, n_kv, d, keys, keys, n_new, seed=9)
+    q[:] = 0xC080  # -4
+    cache["k_scales"][:, :n] = 252
+    cache["k_codes"][:, :n] = 0x77
+    k, v = (x[:, n:] for x in base.held(cache, keys))
+    ref = oracle.decode4_ref(q, k, v, causal=0, bound=True)
+    check(f"no weight {shape}", base.run(q, cache, n_kv, keys, keys, 0), ref, keys, d, 1e-5)
+    cache["v_scales"][:, n // 2, 1] = 255
+    o, lse = base.run(q, cache, n_kv, keys, keys, 0)
+    nan = np.zeros(o.shape, bool)
+    nan[..., 32:64] = True
+    assert np.array_equal(np.isnan(o), nan)
+    check(f"no weight, NaN {shape}", (np.where(nan, ref[0], o), lse), ref, keys, d, 1e-5)
