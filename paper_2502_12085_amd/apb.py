@@ -410,9 +410,10 @@ def layer_fwd(problem, weights: dict, hidden_in, positions, k_cache, v_cache, pa
     _check(st, "apb_layer_fwd")
 
 
-# The elements that a call's sizes ask of each tensor are counted here: a cache
-# is sized by its capacity, not by the rows in use, so a tensor of another size
-# is an easy mistake, and one that the C call cannot see.  Nor can it see a tensor
+# The elements that a call's sizes ask of each tensor are counted here (its shape is
+# its own: a flat buffer in the documented order will do): a cache is sized by its
+# capacity, not by the rows in use, so a tensor of another size is an easy mistake,
+# and one that the C call cannot see.  Nor can it see a tensor
 # of another device than the current one, whose stream the call would use.  A call
 # on a few rows takes 2 us of the GPU, so what the host does is what it costs: a
 # tensor that is as it should be is one expression, and what is wrong is found after.
@@ -456,7 +457,9 @@ def _rows4(t, name, n, dev, validate, problem, where):
 
 
 def _cache4(cache, dev, validate, problem, where):
-    """``apb_cache4_t`` of a mapping of the four tensors (uint8)."""
+    """``apb_cache4_t`` of a mapping of the four tensors (uint8); None for None."""
+    if cache is None:
+        return None
     rows, d, u8 = problem.n_kv_heads * problem.capacity, problem.head_dim, _Cuda.u8
     codes, scales = rows * (d // 2), rows * (d // 32)
     kc, ks, vc, vs = (cache["k_codes"], cache["k_scales"], cache["v_codes"], cache["v_scales"])
@@ -469,14 +472,17 @@ def _cache4(cache, dev, validate, problem, where):
             and kc.is_contiguous() and vc.is_contiguous()
             and ks.is_contiguous() and vs.is_contiguous()):
         return Cache4(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr())
+    # a call that moves or sees no rows takes None in place of any of them
+    idle = 0 == (problem.n_rows if validate is validate_cache4 else problem.cache_len)
     for name, n in (("k_codes", codes), ("k_scales", scales), ("v_codes", codes),
                     ("v_scales", scales)):
         t = cache[name]
         if t is None:
-            _check(validate(problem) or 1, where)
-        if not (t.dtype is u8 and t.numel() == n and t.get_device() == dev
+            _check(validate(problem) or (0 if idle else 1), where)
+        elif not (t.dtype is u8 and t.numel() == n and t.get_device() == dev
                 and t.is_contiguous()):
             _wrong(t, name, (u8,), n, dev, validate(problem), where)
+    return Cache4(*(None if t is None else t.data_ptr() for t in (kc, ks, vc, vs)))
 
 
 def _stream4(stream, dev):
@@ -492,7 +498,8 @@ def validate_cache4(problem) -> int:
 def cache4_write(problem, k, v, cache: dict, stream=None):
     """``apb_cache4_write``: quantise rows of ``k``/``v`` [n_kv, bf16_rows, d]
     (bf16) into ``cache``, a mapping of ``k_codes``/``v_codes`` [n_kv, capacity,
-    d / 2] and ``k_scales``/``v_scales`` [n_kv, capacity, d / 32] (uint8)."""
+    d / 2] and ``k_scales``/``v_scales`` [n_kv, capacity, d / 32] (uint8).  Every
+    tensor may be None when n_rows is 0, the mapping too."""
     dev, where = _device(), "apb_cache4_write"
     n = problem.n_kv_heads * problem.bf16_rows * problem.head_dim
     st = lib().apb_cache4_write(problem, _rows4(k, "k", n, dev, validate_cache4, problem, where),
@@ -531,8 +538,8 @@ def decode4_workspace_size(problem) -> int:
 def decode4_attention(problem, q, cache: dict, o_part, lse_part, workspace, softmax_scale=0.0,
                       stream=None):
     """``apb_decode4_attention``: one host's stage-2 partial attention over a KV
-    cache in 4 bits (``cache`` as in ``cache4_write``; may be None when cache_len
-    is 0).  ``workspace`` is a device tensor of at least
+    cache in 4 bits (``cache`` as in ``cache4_write``; it and its tensors may be
+    None when cache_len is 0).  ``workspace`` is a device tensor of at least
     ``decode4_workspace_size`` bytes (any dtype)."""
     dev, where = _device(), "apb_decode4_attention"
     if workspace is None or workspace.get_device() != dev or not workspace.is_contiguous():
@@ -554,7 +561,7 @@ def decode4_attention(problem, q, cache: dict, o_part, lse_part, workspace, soft
                 _wrong(t, name, (f32,), size, dev, status, where)
     st = lib().apb_decode4_attention(
         problem, _rows4(q, "q", n, dev, validate_decode4, problem, where),
-        None if cache is None else _cache4(cache, dev, validate_decode4, problem, where),
+        _cache4(cache, dev, validate_decode4, problem, where),
         o_part.data_ptr(), lse_part.data_ptr(), softmax_scale, workspace.data_ptr(),
         workspace.numel() * workspace.element_size(), _stream4(stream, dev))
     if st:
