@@ -199,3 +199,32 @@ def test_nan_among_keys_without_weight(shape):
     nan[..., 32:64] = True
     assert np.array_equal(np.isnan(o), nan)
     check(f"no weight, NaN {shape}", (np.where(nan, ref[0], o), lse), ref, keys, d, 1e-5)
+
+
+@pytest.mark.parametrize("rows", [(4, 1, 64, 4), (8, 2, 128, 20), (8, 2, 128, 3)])
+def test_the_rows_beside_one_that_overflows(rows):
+    """A key of the largest numbers in one group of 32, where all queries but two are zero:
+    32 products of 2^129 and more are a NaN for the first, a key without weight for the
+    last, and a logit like another for the rows between."""
+    need_gpu()
+    say(f"[decode4 beside overflow] {rows}")
+    n_q, n_kv, d, n_new = rows
+    keys, at = 300, 77
+    q, cache = base.make(n_q, n_kv, d, keys, keys, n_new, seed=15)
+    q[:, :, :32] = 0
+    q[0, 0, :32], q[-1, -1, :32] = 0x4080, 0xC080  # 4 and -4
+    cache["k_scales"][:, at, 0] = 252
+    cache["k_codes"][:, at, :16] = 0x77
+    o, lse = base.run(q, cache, n_kv, keys, keys, 0)
+    assert np.isnan(o[0, 0]).all() and np.isnan(lse[0, 0])
+    k, v = base.held(cache, keys)
+    q[0, 0, :32] = q[-1, -1, :32] = 0
+    ref = oracle.decode4_ref(q, k, v, causal=0, bound=True)
+    between = np.ones((n_q, n_new), bool)
+    between[0, 0] = between[-1, -1] = False
+    check(f"beside {rows}", (o[between], lse[between]), [x[between] for x in ref], keys, d, 1e-6)
+    # the last without the key (its other logits carry the -4)
+    q[-1, -1, :32] = 0xC080
+    ref = oracle.decode4_ref(q, *(np.delete(x, at, axis=1) for x in (k, v)), causal=0, bound=True)
+    check(f"without the key {rows}", (o[-1:, -1:], lse[-1:, -1:]), [x[-1:, -1:] for x in ref], keys,
+          d, 1e-5)
