@@ -528,7 +528,7 @@ __global__ void __launch_bounds__(kMergeThreads) decode4_merge_kernel(
       const int s = s0 + u * G;
       const size_t at = (size_t)min(s, n_split - 1) * rows + row;
       ms[u] = part_m[at];
-      ls[u] = part_l[at];
+      ls[u] = s < n_split ? part_l[at] : 0.f;
       x[u] = *reinterpret_cast<const f32x4*>(part_o + at * D + 4 * c);
     }
     float m_new = m;
@@ -540,7 +540,6 @@ __global__ void __launch_bounds__(kMergeThreads) decode4_merge_kernel(
     m = m_new;
 #pragma unroll
     for (int u = 0; u < U; ++u) {  // (l = 0: no key with weight; a NaN of V stays)
-      if (s0 + u * G >= n_split) continue;
       const float w = ls[u] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[u] - m);
       acc += w * x[u];
       l = fmaf(w, ls[u], l);
