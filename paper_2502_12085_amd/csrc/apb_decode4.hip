@@ -502,11 +502,10 @@ __global__ void __launch_bounds__(64 * WK, 2) decode4_kernel(Dec4Params p) {
 // the largest m_s; lse = ln 2 (m + log2 l).  Parts keep O undivided, and m apart from
 // log l: a sum of the two would lose l's digits beside a large m.  16 bytes of O a
 // thread; a row's G thread groups take every G-th split, eight at a time against their own
-// maximum, so that all a thread reads is one trip to memory, and meet in LDS.  With few
-// splits one or two groups a row do, and a workgroup has several rows (256 rows of a KV
-// head, 8 heads x 16448 keys, 4 splits: 38.2 -> 36.6 us in all; 128 rows x 4000 keys 14.3 ->
-// 13.3); calls of fewer rows than the GPU has CUs keep a row a workgroup (80 rows 7.5
-// against 7.8).
+// maximum, so that all a thread reads is one trip to memory, and meet in LDS.  With up to
+// 8 or 16 splits one or two groups a row do, and a workgroup has several rows: 256 rows of
+// a KV head, 8 heads x 16448 keys, 4 splits 41.2 -> 40.0 us in all, 128 rows x 4000 keys
+// 14.9 -> 14.0, one row x 1000 7.0 -> 6.3, 40 rows of 2 heads of d = 64 x 1000 7.3 -> 6.4.
 constexpr int kMergeThreads = 256;
 
 template <int D, int G>
@@ -599,9 +598,8 @@ hipError_t launch_d(const Dec4Params& p, const Decode4Plan& pl, hipStream_t stre
                        dim3(kMergeThreads), 0, stream, p.n_split, p.rows_total, p.part_o, p.part_m,
                        p.part_l, p.o, p.lse);
   };
-  const bool many = p.rows_total >= kCus;
-  if (many && pl.n_split <= 8) merge(std::integral_constant<int, 1>{});
-  else if (many && pl.n_split <= 16) merge(std::integral_constant<int, 2>{});
+  if (pl.n_split <= 8) merge(std::integral_constant<int, 1>{});
+  else if (pl.n_split <= 16) merge(std::integral_constant<int, 2>{});
   else merge(std::integral_constant<int, kMergeThreads / (D / 4)>{});
   return hipGetLastError();
 }

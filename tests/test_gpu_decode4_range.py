@@ -48,6 +48,7 @@ SINKS = [
     (32, 8, 128, 16390, 16385, 1, 1),
     (4, 1, 64, 2000, 1999, 7, 1),
     (8, 1, 128, 2000, 1777, 4, 0),
+    (7, 1, 128, 1810, 1800, 1, 1),
     (8, 1, 64, 50000, 49000, 5, 1),
     (8, 1, 128, 50000, 49000, 5, 0),
     (32, 8, 128, 2200, 2112, 64, 1),
