@@ -17,9 +17,11 @@
 // Both directions are bound by HBM: 2 bytes of bf16 and 17 / 32 of cache an element.
 // A thread takes 8 elements (16 bytes of bf16, 4 of codes), a group is four threads.
 // The bf16 side passes the caches by, which leaves them to the cache's codes.  131072 rows
-// of 8 heads of d = 128 (679 MB): write 121 -> 113 us (6.0 TB/s), read 121 -> 106 (6.4),
-// against four rows a thread and plain loads and stores; eight rows 128 and 127, one 114
-// and 130.  A few rows are one launch's latency, 2.4 us.
+// of 8 heads of d = 128 (679 MB), four sets of tensors in turn: write 122 -> 116 us (5.9
+// TB/s), read 123 -> 107 (6.4), against four rows a thread and plain loads and stores;
+// eight rows 120 and 121, one 116 and 128.  (A write and a read of the same rows in turn
+// take 104 and 93: part of the codes is still in the Infinity Cache.)  A few rows are one
+// launch's latency, 1.6 us.
 #include "apb_internal.h"
 
 namespace apb {

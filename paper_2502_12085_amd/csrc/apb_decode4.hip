@@ -7,8 +7,9 @@
 // vector instructions a block to turn codes into operands and to form the softmax.
 // Many rows: the SIMDs' vector instructions, of which a matrix product takes up as
 // much as two (8 cycles of issue whatever its size, 4.7 for an instruction, 8 for a
-// conversion of two codes, 16 for an exponential): 1800 cycles a block of 32 rows, the
-// matrix pipe 1000 of them.  So:
+// conversion of two codes, 16 for an exponential).  A block of 32 rows has 32 products, 64
+// conversions, 16 exponentials and 140 others: 1700 cycles, the matrix pipe busy in 1000 of
+// them, and takes a SIMD's two waves 2250 (512 rows of 8 heads x 16385 keys).  So:
 //  * A wave owns N = 16 or 32 rows and takes 32-key blocks; the waves of a workgroup
 //    share a split's blocks and meet in LDS at its end, so that a split is one partial.
 //  * S^T = K Q^T on v_mfma_f32_16x16x32_bf16 or v_mfma_f32_32x32x16_bf16 (keys on M,

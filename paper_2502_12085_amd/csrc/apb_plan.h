@@ -163,10 +163,11 @@ struct Decode4Plan {
 };
 
 // Most key blocks of a call that is one launch, the waves of one workgroup per KV head
-// and row block sharing them: up to there it takes as long as two launches on the GPU, and
-// the host is 2 us quicker.  16 rows of d = 128: 10 blocks 6.5 -> 5.3 us, 19 6.7 against
-// 6.8; d = 64: 10 5.8 -> 3.9, 17 6.1 -> 4.9, 32 5.9 against 6.2; 32 rows: 10 9.0 -> 9.0,
-// 19 9.2 against 10.8.
+// and row block sharing them: up to there it takes about as long as two launches on the
+// GPU, and the host is 2 us quicker.  Two launches against one, 16 rows of d = 128: 10 blocks
+// 6.2 us against 5.1, 19 6.2 against 6.3, 24 6.0 against 7.1, 32 6.4 against 8.5; d = 64: 10
+// 5.3 against 4.1, 24 5.4 against 5.4, 32 5.3 against 6.1; 32 rows: 10 8.0 against 8.1, 12
+// 8.3 against 8.2, 19 8.1 against 9.7.
 constexpr int decode4_one_launch_blocks(int rows) { return rows == 16 ? 24 : 12; }
 
 inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t cache_len,
@@ -182,8 +183,8 @@ inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t
     if (nblk > 4) pl.waves = 8;
   } else if (pl.rows == 16) {
     // Two workgroups of four waves a CU; or one of eight, which have a block each in half a
-    // round at least: as many waves, half the partials (8 heads: 16385 keys 12.3 -> 11.6
-    // us, 4097 8.7 -> 8.5; 2048 7.4 against 8.3).
+    // round at least: as many waves, half the partials (8 heads: 16385 keys 11.9 -> 11.3
+    // us, 4097 8.4 against 8.4; 2048 7.2 against 7.6).
     const int64_t per_cu = kCus / base;
     if (per_cu > 0 && nblk >= 4 * per_cu) {
       pl.waves = 8;
@@ -193,9 +194,9 @@ inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t
     }
   } else {
     // The splits that make one, two, .. rounds of a workgroup a CU, by what they cost in
-    // blocks of eight waves (1.55 us): a workgroup's own blocks, its start and end (3.5), and
+    // blocks of eight waves (1.8 us): a workgroup's own blocks, its start and end (3.5), and
     // the partials (1.75 and their bytes).  320 row blocks of 250 key blocks (40 / 8 heads,
-    // 256 tokens) 92.5 us in one split, 90.9 so.
+    // 256 tokens) 108.8 us in one round's split, 97.2 so.
     double best = 0;
     for (int64_t r = 1; r <= 6; ++r) {
       const int64_t n = std::max<int64_t>(std::min(kCus * r / base, most), 1);
@@ -209,7 +210,7 @@ inline Decode4Plan plan_decode4(int64_t n_q, int64_t n_kv, int head_dim, int64_t
       }
     }
     // one round of eight waves where they have three blocks each (256 rows of 8 heads x
-    // 16448 keys 43.0 -> 37.1 us, x 4000 18.3 -> 18.0; 40 rows x 4000 11.1 against 12.0),
+    // 16448 keys 46.2 -> 40.4 us, x 4000 18.5 -> 17.4; 40 rows x 4000 11.4 against 12.2),
     // else of four, two workgroups a CU where there are as many
     if (base * n_split <= kCus && nblk >= 24 * n_split) pl.waves = 8;
   }
